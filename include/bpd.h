@@ -304,6 +304,121 @@ int bpd_op_linear(const void* x, const void* w, const void* bias, int rows, int 
                   int dtype, int relu, void* scratch, size_t scratch_bytes, float* y,
                   void* cuda_stream);
 
+/* ---- operators on a paged cache --------------------------------------------
+ *
+ * For programs that keep caches of their own and draft more than a block: trees
+ * of proposals (Section 4's heads rank several candidates each), caches bounded
+ * by a budget, and caches so long that a step reads a part of them.  The cache
+ * has the layout of the decoding path: pages of 64 positions, one pool per
+ * layer, one page table for all layers.
+ *
+ * All of these calls only enqueue work on cuda_stream: they may be captured into
+ * a graph, and keep nothing between calls.  A scratch belongs to one call until
+ * that call's kernels are done (calls on one stream may share one if they are
+ * enqueued one after the other).  Kernels trust no value in a device array: a
+ * length outside [0, capacity] is clamped to it, a node count to [0, nodes], a
+ * parent that does not lie before its node is taken as -1, and a page outside
+ * [0, n_pages) is no page: its positions count as masked and are not written.
+ * Two table entries of different rows may name the same page as long as no call
+ * writes a position of it.  capacity = pages_per_row * 64. */
+typedef struct {
+  void* k_pool;               /* device [layers][n_pages][64][kv_heads][head_dim] of dtype, 16-byte aligned */
+  void* v_pool;               /* the same for the values; may be NULL where a call only reads keys      */
+  const int32_t* page_table;  /* device [batch][pages_per_row]: page of the row's positions 64 p .. 64 p + 63 */
+  int32_t layers;             /* attention and weights calls look at one layer: pass its pools           */
+  int32_t n_pages;
+  int32_t pages_per_row;
+  int32_t batch;
+  int32_t kv_heads;
+  int32_t head_dim;           /* 16, 32, 64 or 128 */
+  int32_t dtype;              /* 0 = float32, 1 = bfloat16; queries, drafted keys and outputs have it too */
+} bpd_cache;
+
+/* Attention of drafted nodes over the cache and their own tree:
+ *   out[b][t] = sum_s softmax_s(scale * q . k_s) v_s,  s in positions [0, lens[b]) and node t's line
+ * where the line of node t is t itself, parents[b][t], and so on up to a node
+ * whose parent is -1 (the last cached token).  parents[b][t] < t; a chain is
+ * parents = t - 1, a single token nodes = 1 and parents = -1.  Queries may have
+ * more heads than the cache: heads is a multiple of kv_heads, and head i reads
+ * key head i / (heads / kv_heads).
+ * q: device [batch * nodes] rows of [heads][head_dim], q_stride elements apart;
+ * k_new, v_new: device [batch * nodes] rows of [kv_heads][head_dim], kv_stride
+ * elements apart (slices of one fused projection will do; rows begin on 16-byte
+ * boundaries).  They are not written to the cache: bpd_op_tree_commit does that
+ * for the accepted ones.  n_nodes: device [batch] or NULL: row b has the first
+ * n_nodes[b] nodes; behind them the outputs are 0 and lse is -inf.  1 <= nodes
+ * <= 256.  out: device [batch][nodes][heads][head_dim] of dtype.  lse: device
+ * float [batch][nodes][heads] or NULL: log of the softmax's sum. */
+size_t bpd_op_tree_attention_scratch_bytes(const bpd_cache* cache, int nodes, int heads);
+int bpd_op_tree_attention(const bpd_cache* cache, const void* q, const void* k_new, const void* v_new, int nodes, int heads,
+                          int64_t q_stride, int64_t kv_stride, const int32_t* lens, const int32_t* parents,
+                          const int32_t* n_nodes, float scale, void* scratch, size_t scratch_bytes, void* out, float* lse,
+                          void* cuda_stream);
+
+/* Verify and commit for trees (Section 3's Verify and Accept with several
+ * candidates per position).  From the last cached token on, the walk goes to the
+ * lowest child whose token is the base model's prediction (last_top1[b] for the
+ * first step, top1[b][node] after), until there is none, the cache is full, or
+ * a token equal to eos_id (>= 0) has been taken.  The path's keys and values go
+ * to positions lens[b], lens[b] + 1, ... of every layer.
+ * k_new, v_new: device [layers][batch][nodes] rows, kv_stride elements apart.
+ * tokens, top1, parents: device [batch][nodes].  Outputs, device int32:
+ * out_lens [batch] (not the array lens), out_accepted [batch], out_path
+ * [batch][nodes] (the nodes taken, -1 behind them), out_next [batch]: the
+ * prediction after the last node taken, i.e. the next step's last_top1. */
+int bpd_op_tree_commit(const bpd_cache* cache, const void* k_new, const void* v_new, int nodes, int64_t kv_stride,
+                       const int32_t* lens, const int32_t* parents, const int32_t* tokens, const int32_t* top1,
+                       const int32_t* last_top1, const int32_t* n_nodes, int32_t eos_id, int32_t* out_lens,
+                       int32_t* out_accepted, int32_t* out_path, int32_t* out_next, void* cuda_stream);
+
+/* Attention weight that the accepted nodes gave to every cached position, added
+ * up: for node path[b][i], i < accepted[b], which sits at position lens[b] + i by
+ * now (lens as before the commit), and positions s <= lens[b] + i,
+ *   weights[b][h][s] += sum over the heads of key head h of exp(scale * q . k_s - lse).
+ * Entries of this commit (s >= lens[b]) start from 0, and positions[b][h][s] is
+ * set to seen[b] + s - lens[b], where seen[b] is the number of tokens committed
+ * before, evicted ones included.  Everything else is left as it was.
+ * q, lse: as given to and returned by the attention.  weights: device float
+ * [batch][kv_heads][capacity]; positions: device int32 of the same shape. */
+int bpd_op_cache_weights(const bpd_cache* cache, const void* q, int nodes, int heads, int64_t q_stride, const float* lse,
+                         const int32_t* path, const int32_t* accepted, const int32_t* lens, const int32_t* seen, float scale,
+                         float* weights, int32_t* positions, void* cuda_stream);
+
+/* Eviction: of every list (layer, row, key head) longer than budget, budget
+ * entries stay -- those with positions >= seen[b] - recent (the last `recent`
+ * tokens), then the largest weights (equal ones: the lower slot; NaN counts as
+ * the smallest).  Survivors keep their slots below budget; the holes there, in
+ * ascending order, take the survivors above, in ascending order: keys, values,
+ * weights and positions move together, what lies at slots >= budget is left as
+ * it was.  Slots are then in no order, which attention does not mind and
+ * `positions` records.  1 <= budget, 0 <= recent <= budget.
+ * weights, positions: device [layers][batch][kv_heads][capacity].  out_lens:
+ * device [batch] (not the array lens): min(lens, budget). */
+size_t bpd_op_cache_evict_scratch_bytes(const bpd_cache* cache, int budget);
+int bpd_op_cache_evict(const bpd_cache* cache, const int32_t* lens, const int32_t* seen, int budget, int recent,
+                       float* weights, int32_t* positions, void* scratch, size_t scratch_bytes, int32_t* out_lens,
+                       void* cuda_stream);
+
+/* Means of the keys of the pages that became full between lens_from[b] and
+ * lens[b] (both device [batch]): means[l][b][p][h][:], device float
+ * [layers][batch][pages_per_row][kv_heads][head_dim].  Sums are in 64 bits and
+ * rounded once.  Other entries are left as they were. */
+int bpd_op_page_means(const bpd_cache* cache, const int32_t* lens_from, const int32_t* lens, float* means, void* cuda_stream);
+
+/* bpd_op_tree_attention over a part of the cache: every node and key head sees
+ * the `select` full pages whose mean key scores highest against the sum of its
+ * group's queries (scores in 64 bits; equal ones: the lower page; NaN counts as
+ * the smallest), the positions behind the last full page, and the node's line.
+ * means: device float [batch][pages_per_row][kv_heads][head_dim] of this layer.
+ * 1 <= select <= pages_per_row.  pages: device int32 [batch][nodes][kv_heads]
+ * [select] or NULL: the selected pages (indices into the row's table), ascending,
+ * -1 behind the last. */
+size_t bpd_op_page_attention_scratch_bytes(const bpd_cache* cache, int nodes, int heads, int select);
+int bpd_op_page_attention(const bpd_cache* cache, const float* means, const void* q, const void* k_new, const void* v_new,
+                          int nodes, int heads, int64_t q_stride, int64_t kv_stride, const int32_t* lens, const int32_t* parents,
+                          const int32_t* n_nodes, int select, float scale, void* scratch, size_t scratch_bytes, void* out,
+                          float* lse, int32_t* pages, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

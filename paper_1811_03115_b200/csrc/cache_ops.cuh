@@ -1,0 +1,518 @@
+// Operators on a paged cache beside its attention: commit of an accepted path, accumulated attention weights, eviction,
+// page means, selection of pages.
+#pragma once
+#include "attention.cuh"
+#include "cache_index.hpp"
+
+namespace bpd {
+namespace tree {
+
+__device__ __forceinline__ unsigned long long order_bits64(double v) {
+  const unsigned long long b = (unsigned long long)__double_as_longlong(v);
+  return (b >> 63) ? ~b : (b | (1ull << 63));
+}
+
+// ------------------------------------------------------------------ commit of the accepted path
+struct CommitArgs {
+  const void *k_new, *v_new;          // [layers][B][T] rows of Hkv * D, kv_stride elements apart
+  void *k_pool, *v_pool;              // [layers][n_pages][64][Hkv * D]
+  const int *table, *lens, *parents, *tokens, *top1, *last_top1, *nodes;
+  int layers, B, T, row_pieces, ppr, n_pages, eos, elem;   // row_pieces: 16-byte pieces of a position's keys
+  long long kv_stride;
+  int *out_lens, *accepted, *path, *next;
+};
+
+// grid (B, splits).  Every CTA walks the tree itself (a few steps over arrays in shared memory), then copies its share of
+// the accepted rows; the first CTA of a sequence writes the walk down.  Bound by launch and walk latency: a batch of 24
+// over 24 layers moves 19 MB.
+constexpr int kCommitThreads = 256;
+__global__ void __launch_bounds__(kCommitThreads) tree_commit_kernel(const __grid_constant__ CommitArgs a) {
+  __shared__ int s_parent[kMaxNodes], s_token[kMaxNodes], s_top1[kMaxNodes], s_path[kMaxNodes], s_row[kMaxNodes], s_n;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
+  const int nodes = a.nodes ? clamp_int(a.nodes[b], 0, a.T) : a.T;
+  const int len = a.lens[b], room = (len < 0 || len > a.ppr * kPagePos) ? 0 : a.ppr * kPagePos - len;
+  for (int i = tid; i < nodes; i += kCommitThreads) {
+    s_parent[i] = a.parents[(long long)b * a.T + i];
+    s_token[i] = a.tokens[(long long)b * a.T + i];
+    s_top1[i] = a.top1[(long long)b * a.T + i];
+  }
+  __syncthreads();
+  if (tid < 32) {
+    int at = -1, want = a.last_top1[b], n = 0;
+    while (n < room) {
+      // the lowest child that carries the wanted token; children lie behind their parent, so the walk ends
+      int child = -1;
+      for (int i0 = (at + 1) & ~31; i0 < nodes; i0 += 32) {
+        const int i = i0 + lane;
+        const unsigned hit = __ballot_sync(0xffffffffu, i < nodes && i > at && parent_of(s_parent[i < nodes ? i : 0], i) == at && s_token[i < nodes ? i : 0] == want);
+        if (hit) { child = i0 + __ffs(hit) - 1; break; }
+      }
+      if (child < 0) break;
+      if (lane == 0) {
+        const int pos = len + n;
+        s_path[n] = child;
+        s_row[n] = (int)pool_row(a.table[(long long)b * a.ppr + pos / kPagePos], a.n_pages, pos);
+      }
+      ++n;
+      at = child;
+      want = s_top1[child];
+      if (a.eos >= 0 && s_token[child] == a.eos) break;
+    }
+    if (lane == 0) {
+      s_n = n;
+      if (blockIdx.y == 0) {
+        a.out_lens[b] = len + n;
+        a.accepted[b] = n;
+        a.next[b] = want;
+      }
+    }
+  }
+  __syncthreads();
+  const int n = s_n;
+  if (blockIdx.y == 0)
+    for (int i = tid; i < a.T; i += kCommitThreads) a.path[(long long)b * a.T + i] = i < n ? s_path[i] : -1;
+  const int per_layer = 2 * n * a.row_pieces, total = a.layers * per_layer;
+  for (int i = blockIdx.y * kCommitThreads + tid; i < total; i += gridDim.y * kCommitThreads) {
+    const int layer = i / per_layer, rest = i % per_layer, which = rest / (n * a.row_pieces), j = rest / a.row_pieces % n, piece = rest % a.row_pieces;
+    if (s_row[j] < 0) continue;
+    const long long per = 16 / a.elem;
+    const long long from = (((long long)layer * a.B + b) * a.T + s_path[j]) * a.kv_stride + piece * per;
+    const long long to = ((long long)layer * a.n_pages * kPagePos + s_row[j]) * a.row_pieces + piece;
+    const char* src = reinterpret_cast<const char*>(which ? a.v_new : a.k_new) + from * a.elem;
+    reinterpret_cast<uint4*>(which ? a.v_pool : a.k_pool)[to] = *reinterpret_cast<const uint4*>(src);
+  }
+}
+
+// ------------------------------------------------------------------ accumulated attention weights
+struct WeightArgs {
+  const void *q, *k_pool;
+  const float* lse;                    // [B][T][H]
+  const int *path, *accepted, *lens, *seen, *table;
+  int B, T, H, Hkv, G, ppr, n_pages;
+  long long q_stride;
+  float scale;
+  float* weights;                      // [B][Hkv][ppr * 64]
+  int* positions;
+};
+
+// weights[s] += sum over accepted nodes i and heads of exp(scale q . k_s - lse), s <= len + i.
+//
+// A product with keys on M and (node, head) rows on N whose result is summed over N: no key depends on another, so a warp
+// streams 16 keys straight from global memory into fragments (the order of the products' k is free as long as both operands
+// agree: a thread takes 16 contiguous bytes) and no key passes through shared memory.  Queries are staged once per CTA.
+// grid (B * Hkv, page groups).  Bound by reading the keys.
+constexpr int kWThreads = 256, kWPages = 8;
+template <typename CT, int D>
+struct WShape {
+  static constexpr bool F32 = sizeof(CT) == 4;
+  static constexpr int PLANES = F32 ? 3 : 1;
+  static constexpr int VEC = D >= 32 ? 8 : 4;                      // elements of k a thread takes at once
+  static constexpr int STEPS = D / (VEC * 4);                      // such takes per key
+  static constexpr int QP = D >= 64 ? D + 32 : (D == 32 ? 32 : 24);   // bf16 elements: two rows' pieces in different banks
+  static constexpr int ROWS = F32 ? 32 : 64;                       // (node, head) rows staged at a time
+};
+template <typename CT, int D>
+__global__ void __launch_bounds__(kWThreads) cache_weights_kernel(const __grid_constant__ WeightArgs a) {
+  using W = WShape<CT, D>;
+  constexpr int VEC = W::VEC, PL = W::PLANES;
+  __shared__ __align__(16) bf16 s_q[PL * W::ROWS * W::QP];
+  __shared__ float s_lse[W::ROWS];
+  __shared__ int s_step[W::ROWS];                                  // index on the path: the row sees positions <= len + it
+  const int b = blockIdx.x / a.Hkv, h = blockIdx.x % a.Hkv, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+  const int cap = a.ppr * kPagePos, len = clamp_int(a.lens[b], 0, cap);
+  const int got = clamp_int(a.accepted[b], 0, min(a.T, cap - len)), total = len + got;
+  if (got == 0 || blockIdx.y * kWPages * kPagePos >= total) return;
+  const int rows = got * a.G;
+  const int p_end = min(ceil_div(total, kPagePos), (int)(blockIdx.y + 1) * kWPages);
+  float* wout = a.weights + ((long long)b * a.Hkv + h) * cap;
+  int* pout = a.positions + ((long long)b * a.Hkv + h) * cap;
+  for (int r0 = 0; r0 < rows; r0 += W::ROWS) {
+    const int n = min(W::ROWS, rows - r0), n8 = (n + 7) & ~7;
+    __syncthreads();
+    for (int i = tid; i < n8 * (D / 4); i += kWThreads) {
+      const int r = i / (D / 4), c = i % (D / 4) * 4;
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      if (r < n) {
+        const int node = clamp_int(a.path[(long long)b * a.T + (r0 + r) / a.G], 0, a.T - 1), head = h * a.G + (r0 + r) % a.G;
+        const CT* src = reinterpret_cast<const CT*>(a.q) + ((long long)b * a.T + node) * a.q_stride + head * D + c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = to_f(src[e]);
+        if (c == 0) { s_lse[r] = a.lse[((long long)b * a.T + node) * a.H + head]; s_step[r] = (r0 + r) / a.G; }
+      } else if (c == 0) {
+        s_lse[r] = INFINITY; s_step[r] = -1;                       // weight 0
+      }
+      if constexpr (W::F32) {
+        uint32_t x[3], y[3];
+        attn::split3_pair(v[0], v[1], x);
+        attn::split3_pair(v[2], v[3], y);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2*>(s_q + (q * W::ROWS + r) * W::QP + c) = make_uint2(x[q], y[q]);
+      } else {
+        *reinterpret_cast<uint2*>(s_q + r * W::QP + c) = make_uint2(attn::pack2(from_f<bf16>(v[0]), from_f<bf16>(v[1])), attn::pack2(from_f<bf16>(v[2]), from_f<bf16>(v[3])));
+      }
+    }
+    __syncthreads();
+    for (int tile = blockIdx.y * kWPages * 4 + warp; tile < p_end * 4; tile += kWThreads / 32) {
+      const int pos0 = tile * 16;
+      if (pos0 >= total) break;
+      const int page = a.table[(long long)b * a.ppr + pos0 / kPagePos];
+      const long long row = pool_row(page, a.n_pages, pos0);
+      const bool ok[2] = {row >= 0 && pos0 + g < total, row >= 0 && pos0 + g + 8 < total};
+      const CT* kp = reinterpret_cast<const CT*>(a.k_pool) + ((row < 0 ? 0 : row) * a.Hkv + h) * D;
+      float sum0 = 0.f, sum1 = 0.f;
+      uint32_t kf[PL][W::STEPS][2][VEC / 2];                       // [plane][take][row half][pairs]
+#pragma unroll
+      for (int st = 0; st < W::STEPS; ++st)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const CT* src = kp + (long long)(g + half * 8) * a.Hkv * D + (t4 + 4 * st) * VEC;
+          if constexpr (W::F32) {
+            float4 v[VEC / 4];
+#pragma unroll
+            for (int e = 0; e < VEC / 4; ++e) v[e] = ok[half] ? reinterpret_cast<const float4*>(src)[e] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int e = 0; e < VEC / 4; ++e) {
+              uint32_t x[3], y[3];
+              attn::split3_pair(v[e].x, v[e].y, x);
+              attn::split3_pair(v[e].z, v[e].w, y);
+#pragma unroll
+              for (int q = 0; q < PL; ++q) { kf[q][st][half][2 * e] = x[q]; kf[q][st][half][2 * e + 1] = y[q]; }
+            }
+          } else if constexpr (VEC == 8) {
+            const uint4 v = ok[half] ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
+            kf[0][st][half][0] = v.x; kf[0][st][half][1] = v.y; kf[0][st][half][2] = v.z; kf[0][st][half][3] = v.w;
+          } else {
+            const uint2 v = ok[half] ? *reinterpret_cast<const uint2*>(src) : make_uint2(0u, 0u);
+            kf[0][st][half][0] = v.x; kf[0][st][half][1] = v.y;
+          }
+        }
+      for (int n0 = 0; n0 < n8; n0 += 8) {
+        float c[4] = {0.f, 0.f, 0.f, 0.f}, lo[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < W::STEPS; ++st) {
+          uint32_t qf[PL][VEC / 2];
+#pragma unroll
+          for (int q = 0; q < PL; ++q) {
+            const bf16* src = s_q + (q * W::ROWS + n0 + g) * W::QP + (t4 + 4 * st) * VEC;
+            if constexpr (VEC == 8) {
+              const uint4 v = *reinterpret_cast<const uint4*>(src);
+              qf[q][0] = v.x; qf[q][1] = v.y; qf[q][2] = v.z; qf[q][3] = v.w;
+            } else {
+              const uint2 v = *reinterpret_cast<const uint2*>(src);
+              qf[q][0] = v.x; qf[q][1] = v.y;
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < VEC / 4; ++k)
+#pragma unroll
+            for (int p = 0; p < PL; ++p) {
+              const uint32_t aq[4] = {kf[p][st][0][2 * k], kf[p][st][1][2 * k], kf[p][st][0][2 * k + 1], kf[p][st][1][2 * k + 1]};
+#pragma unroll
+              for (int q = 0; q < PL - p; ++q) attn::mma_bf16(p + q == 0 ? c : lo, aq, qf[q][2 * k], qf[q][2 * k + 1]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int r = n0 + t4 * 2 + (j & 1), pos = pos0 + g + (j < 2 ? 0 : 8);
+          const float w = pos <= len + s_step[r] ? expf(fmaf(c[j] + lo[j], a.scale, -s_lse[r])) : 0.f;
+          if (j < 2) sum0 += w; else sum1 += w;
+        }
+      }
+      sum0 += __shfl_xor_sync(0xffffffffu, sum0, 1); sum0 += __shfl_xor_sync(0xffffffffu, sum0, 2);
+      sum1 += __shfl_xor_sync(0xffffffffu, sum1, 1); sum1 += __shfl_xor_sync(0xffffffffu, sum1, 2);
+      if (t4 < 2) {
+        const int pos = pos0 + g + t4 * 8;
+        const float add = t4 ? sum1 : sum0;
+        if (pos < total) {
+          // entries of this commit begin here: nothing of what the slot held before counts
+          wout[pos] = (pos < len || r0 > 0) ? wout[pos] + (ok[t4] ? add : 0.f) : (ok[t4] ? add : 0.f);
+          if (pos >= len && r0 == 0) pout[pos] = a.seen[b] + pos - len;
+        }
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ eviction
+struct EvictArgs {
+  void *k_pool, *v_pool;               // [layers][n_pages][64][Hkv][D]
+  const int *table, *lens, *seen;
+  int layers, B, Hkv, row_pieces, ppr, n_pages, budget, recent;   // row_pieces: 16-byte pieces of a head's keys
+  float* weights;                      // [layers][B][Hkv][ppr * 64]
+  int* positions;
+  int* out_lens;
+  int* moves;                          // scratch: [layers * B * Hkv][2][min(budget, capacity)] slots: holes, and what fills them
+  int moves_cap;
+};
+
+// Weight as a number whose unsigned order is the order of eviction: NaN below everything, -0 like 0.
+__device__ __forceinline__ unsigned evict_key(float w) { return w != w ? 0u : order_bits(w + 0.f); }
+
+// A CTA per list (layer, sequence, key head): a radix selection over the weights finds the lightest key that stays, ordered
+// scans list the holes below the budget and the survivors above it, then the rows move.  Sources lie at or above the
+// budget, targets below it: no row is read after it was written, in whatever order they move.
+constexpr int kEvictThreads = 512;
+__global__ void __launch_bounds__(kEvictThreads) cache_evict_kernel(const __grid_constant__ EvictArgs a) {
+  __shared__ int s_hist[2048], s_warp[2][kEvictThreads / 32], s_pick[2];
+  const int list = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int h = list % a.Hkv, b = list / a.Hkv % a.B, layer = list / a.Hkv / a.B;
+  const int cap = a.ppr * kPagePos, len = clamp_int(a.lens[b], 0, cap);
+  if (layer == 0 && h == 0 && tid == 0) a.out_lens[b] = min(len, a.budget);
+  if (len <= a.budget) return;
+  float* w = a.weights + (long long)list * cap;
+  int* pos = a.positions + (long long)list * cap;
+  const long long recent_from = (long long)a.seen[b] - a.recent;
+
+  auto block_count = [&](int v) {                          // sum over the block
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();
+    if (lane == 0) s_warp[0][warp] = v;
+    __syncthreads();
+    int sum = 0;
+    for (int i = 0; i < kEvictThreads / 32; ++i) sum += s_warp[0][i];
+    return sum;
+  };
+  int mine = 0;
+  for (int i = tid; i < len; i += kEvictThreads) mine += pos[i] >= recent_from;
+  const int recents = block_count(mine);
+  // the group that the border runs through, and how many of it stay
+  const bool in_recent = recents >= a.budget;
+  int need = in_recent ? a.budget : a.budget - recents;
+  unsigned prefix = 0, prefix_mask = 0;
+  for (int shift = 21; shift >= 0; shift = shift == 21 ? 10 : (shift == 10 ? 0 : -1)) {
+    const int bins = shift == 0 ? 1024 : 2048;
+    for (int i = tid; i < 2048; i += kEvictThreads) s_hist[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < len; i += kEvictThreads) {
+      const unsigned key = evict_key(w[i]);
+      if ((pos[i] >= recent_from) == in_recent && (key & prefix_mask) == prefix) atomicAdd(&s_hist[(key >> shift) & (bins - 1)], 1);
+    }
+    __syncthreads();
+    // the bin, from the heaviest down, in which the count reaches `need`
+    if (warp == 0) {
+      int above = 0;
+      for (int top = bins - 32; top >= 0; top -= 32) {
+        const int n = s_hist[top + 31 - lane];
+        int upto = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += x; }
+        const unsigned hit = __ballot_sync(0xffffffffu, above + upto >= need);
+        if (hit) {
+          const int at = __ffs(hit) - 1;
+          if (lane == at) { s_pick[0] = top + 31 - lane; s_pick[1] = need - (above + upto - n); }
+          break;
+        }
+        above += __shfl_sync(0xffffffffu, upto, 31);
+      }
+    }
+    __syncthreads();
+    prefix |= (unsigned)s_pick[0] << shift;
+    prefix_mask |= (unsigned)(bins - 1) << shift;
+    need = s_pick[1];
+    __syncthreads();
+  }
+  // `prefix` is the border's key, `need` how many entries of that key stay (the lowest slots)
+  int* holes = a.moves + (long long)list * 2 * a.moves_cap;
+  int* fill = holes + a.moves_cap;
+  int ties = 0, n_holes = 0, n_fill = 0;
+  for (int i0 = 0; i0 < len; i0 += kEvictThreads) {
+    const int i = i0 + tid;
+    bool stays = false, tie = false;
+    if (i < len) {
+      const bool rec = pos[i] >= recent_from;
+      if (rec != in_recent) stays = rec;
+      else {
+        const unsigned key = evict_key(w[i]);
+        stays = key > prefix;
+        tie = key == prefix;
+      }
+    }
+    unsigned m = __ballot_sync(0xffffffffu, tie);
+    if (lane == 0) s_warp[0][warp] = __popc(m);
+    __syncthreads();
+    int before = ties, all = 0;
+    for (int k = 0; k < kEvictThreads / 32; ++k) { if (k < warp) before += s_warp[0][k]; all += s_warp[0][k]; }
+    if (tie && before + __popc(m & ((1u << lane) - 1)) < need) stays = true;
+    ties += all;
+    const bool hole = i < a.budget && !stays, filler = i < len && i >= a.budget && stays;   // (i < budget < len)
+    const unsigned mh = __ballot_sync(0xffffffffu, hole), mf = __ballot_sync(0xffffffffu, filler);
+    __syncthreads();
+    if (lane == 0) { s_warp[0][warp] = __popc(mh); s_warp[1][warp] = __popc(mf); }
+    __syncthreads();
+    int bh = n_holes, bf = n_fill;
+    for (int k = 0; k < kEvictThreads / 32; ++k) {
+      if (k < warp) { bh += s_warp[0][k]; bf += s_warp[1][k]; }
+      n_holes += s_warp[0][k]; n_fill += s_warp[1][k];
+    }
+    if (hole) holes[bh + __popc(mh & ((1u << lane) - 1))] = i;
+    if (filler) fill[bf + __popc(mf & ((1u << lane) - 1))] = i;
+    __syncthreads();
+  }
+  __threadfence_block();
+  __syncthreads();
+  const int n = min(n_holes, n_fill);
+  const int* table = a.table + (long long)b * a.ppr;
+  const long long layer_rows = (long long)layer * a.n_pages * kPagePos;
+  for (long long i = tid; i < (long long)n * 2 * a.row_pieces; i += kEvictThreads) {
+    const int j = (int)(i / (2 * a.row_pieces)), rest = (int)(i % (2 * a.row_pieces)), which = rest / a.row_pieces, piece = rest % a.row_pieces;
+    const int to = holes[j], from = fill[j];
+    const long long rt = pool_row(table[to / kPagePos], a.n_pages, to), rf = pool_row(table[from / kPagePos], a.n_pages, from);
+    if (rt < 0 || rf < 0) continue;
+    uint4* pool = reinterpret_cast<uint4*>(which ? a.v_pool : a.k_pool);
+    pool[((layer_rows + rt) * a.Hkv + h) * a.row_pieces + piece] = pool[((layer_rows + rf) * a.Hkv + h) * a.row_pieces + piece];
+  }
+  for (int j = tid; j < n; j += kEvictThreads) {
+    w[holes[j]] = w[fill[j]];
+    pos[holes[j]] = pos[fill[j]];
+  }
+}
+
+// ------------------------------------------------------------------ page means
+struct MeansArgs {
+  const void* k_pool;                  // [layers][n_pages][64][width]
+  const int *table, *from, *lens;
+  int layers, B, width, ppr, n_pages;  // width = Hkv * D
+  float* means;                        // [layers][B][ppr][width]
+};
+
+// Means of the keys of the pages that have become full.  Sums are in 64 bits and rounded once: selections go by them, and
+// a sum whose rounding depends on its order would make near ties depend on it too.  grid (ppr, B, layers), a thread per four
+// columns.
+constexpr int kMeansThreads = 128;
+template <typename CT>
+__global__ void __launch_bounds__(kMeansThreads) page_means_kernel(const __grid_constant__ MeansArgs a) {
+  const int p = blockIdx.x, b = blockIdx.y, layer = blockIdx.z, cap = a.ppr * kPagePos;
+  if (p >= clamp_int(a.lens[b], 0, cap) / kPagePos || p < clamp_int(a.from[b], 0, cap) / kPagePos) return;
+  const int page = a.table[(long long)b * a.ppr + p];
+  const long long row = pool_row(page, a.n_pages, 0);
+  if (row < 0) return;
+  const CT* src = reinterpret_cast<const CT*>(a.k_pool) + ((long long)layer * a.n_pages * kPagePos + row) * a.width;
+  float* out = a.means + (((long long)layer * a.B + b) * a.ppr + p) * a.width;
+  for (int c = threadIdx.x * 4; c < a.width; c += kMeansThreads * 4) {
+    double s[4] = {0., 0., 0., 0.};
+#pragma unroll 8
+    for (int r = 0; r < kPagePos; ++r) {
+      float v[4];
+      if constexpr (sizeof(CT) == 4) {
+        const float4 x = *reinterpret_cast<const float4*>(src + (long long)r * a.width + c);
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+      } else {
+        const uint2 x = *reinterpret_cast<const uint2*>(src + (long long)r * a.width + c);
+        v[0] = __uint_as_float(x.x << 16); v[1] = __uint_as_float(x.x & 0xffff0000u);
+        v[2] = __uint_as_float(x.y << 16); v[3] = __uint_as_float(x.y & 0xffff0000u);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += (double)v[e];
+    }
+    *reinterpret_cast<float4*>(out + c) = make_float4((float)(s[0] / kPagePos), (float)(s[1] / kPagePos), (float)(s[2] / kPagePos), (float)(s[3] / kPagePos));
+  }
+}
+
+// ------------------------------------------------------------------ selection of pages
+struct SelectArgs {
+  const void* q;
+  const float* means;                  // [B][ppr][Hkv][D]
+  const int *lens, *nodes;
+  int B, T, H, Hkv, G, D, ppr, select;
+  long long q_stride;
+  unsigned long long* keys;            // scratch [B][T][Hkv][ppr]
+  int* pages;                          // [B][T][Hkv][select]
+};
+
+// score(page) = (sum of the group's queries) . mean, in 64 bits: the border of a selection is often close.  The best
+// `select` full pages (ties and NaN: the lower page, NaN below everything), listed in ascending order.  A CTA per (node,
+// key head).
+constexpr int kSelectThreads = 256;
+template <typename CT>
+__global__ void __launch_bounds__(kSelectThreads) page_select_kernel(const __grid_constant__ SelectArgs a) {
+  __shared__ double s_q[128];
+  __shared__ int s_hist[256], s_warp[kSelectThreads / 32], s_pick[2];
+  const int id = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int h = id % a.Hkv, t = id / a.Hkv % a.T, b = id / a.Hkv / a.T;
+  int* out = a.pages + (long long)id * a.select;
+  const int full = clamp_int(a.lens[b], 0, a.ppr * kPagePos) / kPagePos;
+  const bool alive = !a.nodes || t < a.nodes[b];
+  const int n_out = alive ? min(full, a.select) : 0;
+  for (int i = n_out + tid; i < a.select; i += kSelectThreads) out[i] = -1;
+  if (n_out == 0) return;
+  if (full <= a.select) {
+    for (int i = tid; i < full; i += kSelectThreads) out[i] = i;
+    return;
+  }
+  for (int d = tid; d < a.D; d += kSelectThreads) {
+    double s = 0.;
+    const CT* src = reinterpret_cast<const CT*>(a.q) + ((long long)b * a.T + t) * a.q_stride + h * a.G * a.D + d;
+    for (int g = 0; g < a.G; ++g) s += (double)to_f(src[g * a.D]);
+    s_q[d] = s;
+  }
+  __syncthreads();
+  unsigned long long* keys = a.keys + (long long)id * a.ppr;
+  for (int p = warp; p < full; p += kSelectThreads / 32) {
+    const float* m = a.means + (((long long)b * a.ppr + p) * a.Hkv + h) * a.D;
+    double s = 0.;
+    for (int d = lane; d < a.D; d += 32) s += s_q[d] * (double)m[d];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == 0) keys[p] = s != s ? 0ull : order_bits64(s + 0.);
+  }
+  __threadfence_block();
+  __syncthreads();
+  unsigned long long prefix = 0, mask = 0;
+  int need = a.select;
+  for (int shift = 56; shift >= 0; shift -= 8) {
+    for (int i = tid; i < 256; i += kSelectThreads) s_hist[i] = 0;
+    __syncthreads();
+    for (int p = tid; p < full; p += kSelectThreads) {
+      const unsigned long long k = keys[p];
+      if ((k & mask) == prefix) atomicAdd(&s_hist[(k >> shift) & 255], 1);
+    }
+    __syncthreads();
+    if (warp == 0) {
+      int above = 0;
+      for (int top = 224; top >= 0; top -= 32) {
+        const int n = s_hist[top + 31 - lane];
+        int upto = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += x; }
+        const unsigned hit = __ballot_sync(0xffffffffu, above + upto >= need);
+        if (hit) {
+          const int at = __ffs(hit) - 1;
+          if (lane == at) { s_pick[0] = top + 31 - lane; s_pick[1] = need - (above + upto - n); }
+          break;
+        }
+        above += __shfl_sync(0xffffffffu, upto, 31);
+      }
+    }
+    __syncthreads();
+    prefix |= (unsigned long long)s_pick[0] << shift;
+    mask |= 255ull << shift;
+    need = s_pick[1];
+    __syncthreads();
+  }
+  int ties = 0, done = 0;
+  for (int p0 = 0; p0 < full; p0 += kSelectThreads) {
+    const int p = p0 + tid;
+    const unsigned long long k = p < full ? keys[p] : 0ull;
+    const bool tie = p < full && k == prefix;
+    bool in = p < full && k > prefix;
+    unsigned m = __ballot_sync(0xffffffffu, tie);
+    if (lane == 0) s_warp[warp] = __popc(m);
+    __syncthreads();
+    int before = ties, all = 0;
+    for (int i = 0; i < kSelectThreads / 32; ++i) { if (i < warp) before += s_warp[i]; all += s_warp[i]; }
+    if (tie && before + __popc(m & ((1u << lane) - 1)) < need) in = true;
+    ties += all;
+    m = __ballot_sync(0xffffffffu, in);
+    __syncthreads();
+    if (lane == 0) s_warp[warp] = __popc(m);
+    __syncthreads();
+    int at = done;
+    for (int i = 0; i < kSelectThreads / 32; ++i) { if (i < warp) at += s_warp[i]; done += s_warp[i]; }
+    if (in) out[at + __popc(m & ((1u << lane) - 1))] = p;
+    __syncthreads();
+  }
+}
+
+}  // namespace tree
+}  // namespace bpd

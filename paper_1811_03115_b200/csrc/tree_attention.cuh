@@ -1,0 +1,622 @@
+// Attention of drafted nodes over a paged cache and over their own tree.
+//
+//   out[t] = sum_s softmax_s(scale q_t . k_s) v_s,   s in {cached positions} + {ancestors of t and t itself}
+//
+// Either every cached position below the sequence's length counts (dense), or the pages that were selected for the node and
+// key head, plus the open page (paged).  One kernel for both: a tile of query rows (nodes x heads of a key head's group when
+// dense; the heads of the group of one node when paged) walks chunks of 64 keys -- a page is a chunk, so a chunk has one
+// table entry -- with the running maximum and sum of the softmax in registers.  Scores and outputs are mma.sync products.
+//
+// Work is cut by chunks, not by tiles: the chunks of all tiles of all sequences are laid end to end and every CTA takes an
+// equal run of them, so ragged batches and single long sequences fill the device alike.  A run that begins or ends inside a
+// tile leaves a partial result (maximum, sum, unnormalised output) in the scratch; combine_kernel joins those.
+//
+// Precision: bf16 caches: scores are exact products summed in fp32; softmax weights go into the second product as two bf16
+// planes (w = h + l, 16 bits of mantissa), so the output's error is its own rounding to bf16 (with one plane it was 1.4
+// times that).  fp32 caches: every operand is three bf16 planes (24 bits), the six largest of the nine products are taken
+// (the rest is below 2^-24), and outputs are summed per chunk in the tensor core but across chunks by fp32 FMAs (the tensor
+// core's own additions truncate).
+#pragma once
+#include "attention.cuh"
+#include "cache_index.hpp"
+
+namespace bpd {
+namespace tree {
+
+using attn::cp_async16;
+using attn::ldsm4;
+using attn::mma_bf16;
+using attn::s_addr;
+using attn::split3_pair;
+
+constexpr int kThreads = 128;
+constexpr int kChunk = kPagePos;
+
+struct AttnArgs {
+  const void *q, *k_new, *v_new, *k_pool, *v_pool;
+  const int *table, *lens, *parents, *nodes;   // nodes may be null: T each
+  const int* pages;                            // paged: [B][T][Hkv][select], ascending, -1 behind the last
+  int B, T, H, Hkv, G, ppr, n_pages, select;
+  long long q_stride, kv_stride;               // elements between consecutive nodes
+  float scale_log2;                            // scale * log2(e)
+  void* out;                                   // [B][T][H][D]
+  float* lse;                                  // [B][T][H] or null
+  float* part;                                 // [ctas][2][R * (D + 2)]
+  int2* info;                                  // per tile: 2 * first CTA that has units of it + the slot of its partial result; last CTA
+};
+
+// Shared-memory layout of a chunk's rows.  bf16: 16-byte pieces, XOR-swizzled so that eight consecutive rows' same piece
+// lies in eight different 16-byte columns of the banks; fp32: padded rows (see attention.cuh).
+template <typename CT, int D>
+struct Rows {
+  static constexpr bool F32 = sizeof(CT) == 4;
+  static constexpr int PIECES = D * (int)sizeof(CT) / 16;
+  static constexpr int PER = 16 / (int)sizeof(CT);
+  static constexpr int KP = D + 8, VP = D + 4;             // fp32 pitches (floats)
+  static constexpr int K_BYTES = F32 ? kChunk * KP * 4 : kChunk * D * 2;
+  static constexpr int V_BYTES = F32 ? kChunk * VP * 4 : kChunk * D * 2;
+  static constexpr int STAGE = K_BYTES + V_BYTES;
+  __device__ __forceinline__ static uint32_t swz(int row, int piece) {
+    constexpr int PER_LINE = PIECES >= 8 ? 1 : 8 / PIECES, MASK = PIECES >= 8 ? 7 : PIECES - 1;
+    return (uint32_t)(row * PIECES + (piece ^ ((row / PER_LINE) & MASK))) * 16u;
+  }
+  __device__ __forceinline__ static uint32_t k_at(int row, int piece) { return F32 ? (uint32_t)(row * KP + piece * 4) * 4u : swz(row, piece); }
+  __device__ __forceinline__ static uint32_t v_at(int row, int piece) { return F32 ? (uint32_t)(row * VP + piece * 4) * 4u : swz(row, piece); }
+};
+
+// WR warps side by side over rows (16 each), 4 / WR over the keys of a chunk.
+template <typename CT, int D, int WR>
+struct Shape {
+  static constexpr bool F32 = sizeof(CT) == 4;
+  static constexpr int R = 16 * WR, WK = 4 / WR, KW = kChunk / WK;
+  static constexpr int QP = D + 8;                          // pitch of a query plane (bf16 elements), fp32 caches only
+  static constexpr int Q_BYTES = F32 ? 3 * R * QP * 2 : 0;
+  static constexpr int MP = D + 4;                          // pitch of the merge buffer (floats)
+  static constexpr int MERGE = WK * R * MP * 4;
+  static constexpr int STAGES = F32 ? (D >= 128 ? 2 : 3) : (D >= 128 ? 3 : 4);
+  static constexpr int RING = STAGES * Rows<CT, D>::STAGE;
+  static constexpr int SMEM = Q_BYTES + (RING > MERGE ? RING : MERGE);
+  static constexpr int CTAS_PER_SM = F32 ? (D >= 128 ? 1 : 2) : (D >= 128 ? 2 : 3);
+  static constexpr int PART = R * (D + 2);                  // floats of a partial result
+};
+
+// Bits of the ancestors-or-self of node t among nodes 64 * word .. 64 * word + 63.
+__device__ __forceinline__ unsigned long long line_bits(const int* parents, int t, int word) {
+  unsigned long long bits = 0;
+  while (t >= 0) {
+    if ((t >> 6) == word) bits |= 1ull << (t & 63);
+    t = parent_of(parents[t], t);
+  }
+  return bits;
+}
+
+struct Seq { int len, nodes; SeqWork w; };
+
+template <bool PAGED>
+__device__ __forceinline__ Seq seq_of(const AttnArgs& a, int b, int tile_rows) {
+  Seq s;
+  s.len = clamp_int(a.lens[b], 0, a.ppr * kPagePos);
+  s.nodes = a.nodes ? clamp_int(a.nodes[b], 0, a.T) : a.T;
+  s.w = PAGED ? paged_work(s.len, s.nodes, a.select, a.Hkv, a.G, tile_rows) : dense_work(s.len, s.nodes, a.Hkv, a.G, tile_rows);
+  return s;
+}
+
+// Tile `local` of a sequence: node (paged only), key head, first row; and its number among all tiles that could be.
+struct Tile { int t, h, r0, id; };
+template <bool PAGED>
+__device__ __forceinline__ Tile tile_of(const AttnArgs& a, int b, int nodes, int local, int tile_rows) {
+  Tile x;
+  if (PAGED) {
+    const int rt = ceil_div(a.G, tile_rows);
+    x.t = local / (a.Hkv * rt);
+    x.h = local / rt % a.Hkv;
+    x.r0 = local % rt * tile_rows;
+    x.id = ((b * a.T + x.t) * a.Hkv + x.h) * rt + local % rt;
+  } else {
+    const int rt = ceil_div(nodes * a.G, tile_rows), rt_all = ceil_div(a.T * a.G, tile_rows);
+    x.t = 0;
+    x.h = local / rt;
+    x.r0 = local % rt * tile_rows;
+    x.id = (b * a.Hkv + x.h) * rt_all + local % rt;
+  }
+  return x;
+}
+
+template <typename CT> __device__ __forceinline__ void store4(CT* p, float4 v);
+template <> __device__ __forceinline__ void store4<float>(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+template <> __device__ __forceinline__ void store4<bf16>(bf16* p, float4 v) {
+  __nv_bfloat162 x = __floats2bfloat162_rn(v.x, v.y), y = __floats2bfloat162_rn(v.z, v.w);
+  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<uint32_t*>(&x), *reinterpret_cast<uint32_t*>(&y));
+}
+
+// Two floats as two pairs of bf16, high and low.
+__device__ __forceinline__ void split2_pair(float x, float y, uint32_t& hi, uint32_t& lo) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+  hi = *reinterpret_cast<const uint32_t*>(&h);
+  const __nv_bfloat162 l = __floats2bfloat162_rn(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u));
+  lo = *reinterpret_cast<const uint32_t*>(&l);
+}
+
+// Sum over the block; every thread gets it.  `box`: one slot per warp.
+__device__ __forceinline__ long long block_sum(long long v, long long* box) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) box[threadIdx.x >> 5] = v;
+  __syncthreads();
+  return box[0] + box[1] + box[2] + box[3];
+}
+
+template <typename CT, int D, int WR, bool PAGED>
+__global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_constant__ AttnArgs a) {
+  using S = Shape<CT, D, WR>;
+  using L = Rows<CT, D>;
+  pdl_launch_dependents();
+  constexpr bool F32 = S::F32;
+  constexpr int R = S::R, WK = S::WK, KW = S::KW, KT = D / 16, NT = KW / 8, DT = D / 8;
+  extern __shared__ __align__(128) uint8_t ta_smem[];
+  __shared__ long long s_box[4];
+  __shared__ long long s_at;            // first unit of the sequence the CTA begins in
+  __shared__ int s_b, s_keys[S::STAGES], s_parents[kMaxNodes];
+  __shared__ unsigned long long s_line[R][kMaxNodes / 64];
+  __shared__ float s_m[WK][R], s_l[WK][R];
+  bf16* qs = reinterpret_cast<bf16*>(ta_smem);
+  uint8_t* ring = ta_smem + S::Q_BYTES;
+  const uint32_t ring_s = s_addr(ring);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+  const int wr = warp % WR, wk = warp / WR;
+
+  // rows behind a sequence's last node: zeros, and a log-sum of nothing
+  if (a.nodes) {
+    for (int i = blockIdx.x; i < a.B * a.T; i += gridDim.x) {
+      if (i % a.T < clamp_int(a.nodes[i / a.T], 0, a.T)) continue;
+      CT* o = reinterpret_cast<CT*>(a.out) + (long long)i * a.H * D;
+      for (int c = tid * 4; c < a.H * D; c += kThreads * 4) store4<CT>(o + c, make_float4(0.f, 0.f, 0.f, 0.f));
+      if (a.lse) for (int c = tid; c < a.H; c += kThreads) a.lse[(long long)i * a.H + c] = -INFINITY;
+    }
+  }
+
+  // this CTA's run of units, and the sequence it begins in
+  long long mine = 0;
+  for (int b = tid; b < a.B; b += kThreads) { const SeqWork w = seq_of<PAGED>(a, b, R).w; mine += (long long)w.tiles * w.chunks; }
+  const long long units = block_sum(mine, s_box);
+  const long long ctas = min(units, (long long)gridDim.x);  // no CTA that shares a tile may be without a unit
+  if (blockIdx.x >= ctas) return;
+  const long long u_begin = first_unit(blockIdx.x, units, ctas), u_end = first_unit(blockIdx.x + 1, units, ctas);
+  long long before = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+    const int b = b0 + tid;
+    long long n = 0;
+    if (b < a.B) { const SeqWork w = seq_of<PAGED>(a, b, R).w; n = (long long)w.tiles * w.chunks; }
+    long long upto = n;                                     // inclusive scan over the block
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const long long x = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += x; }
+    __syncthreads();
+    if (lane == 31) s_box[warp] = upto;
+    __syncthreads();
+    long long base = before;
+    for (int w = 0; w < warp; ++w) base += s_box[w];
+    if (n > 0 && base + upto - n <= u_begin && u_begin < base + upto) { s_b = b; s_at = base + upto - n; }
+    before += s_box[0] + s_box[1] + s_box[2] + s_box[3];
+    __syncthreads();
+    if (before > u_begin) break;
+  }
+  int b = s_b;
+  long long seq_first = s_at, u = u_begin;
+  Seq sq = seq_of<PAGED>(a, b, R);
+  int lines_of = -1;                                        // sequence whose parents are in shared memory
+
+  while (u < u_end) {
+    while (u >= seq_first + (long long)sq.w.tiles * sq.w.chunks) {
+      seq_first += (long long)sq.w.tiles * sq.w.chunks;
+      sq = seq_of<PAGED>(a, ++b, R);
+    }
+    const int local = (int)((u - seq_first) / sq.w.chunks);
+    const long long tile_first = seq_first + (long long)local * sq.w.chunks;
+    const int c_begin = (int)(u - tile_first), c_end = (int)min((long long)sq.w.chunks, u_end - tile_first);
+    const Tile tl = tile_of<PAGED>(a, b, sq.nodes, local, R);
+    const int rows = PAGED ? min(R, a.G - tl.r0) : min(R, sq.nodes * a.G - tl.r0);
+    const int tree_chunks = ceil_div(sq.nodes, kChunk), cache_chunks = sq.w.chunks - tree_chunks;
+    const int full = sq.len / kPagePos;
+    const int* table = a.table + (long long)b * a.ppr;
+    const int* sel = PAGED ? a.pages + ((long long)(b * a.T + tl.t) * a.Hkv + tl.h) * a.select : nullptr;
+    // node and head of row r of the tile
+    auto node_of = [&](int r) { return PAGED ? tl.t : (tl.r0 + r) / a.G; };
+    auto head_of = [&](int r) { return tl.h * a.G + (PAGED ? tl.r0 + r : (tl.r0 + r) % a.G); };
+
+    // page and keys of cache chunk c (page -1: none)
+    auto page_of = [&](int c) -> int {
+      if (c >= cache_chunks) return -1;
+      int logical = c;
+      if (PAGED && c < cache_chunks - (sq.len % kPagePos ? 1 : 0)) {
+        logical = sel[c];
+        if (logical < 0 || logical >= full) return -1;
+      } else if (PAGED) {
+        logical = full;
+      }
+      const int page = table[logical];
+      return pool_row(page, a.n_pages, 0) < 0 ? -1 : page;
+    };
+    auto keys_of = [&](int c, int page) -> int {
+      if (c >= cache_chunks) return min(kChunk, sq.nodes - (c - cache_chunks) * kChunk);
+      if (page < 0) return 0;
+      const bool open = PAGED ? c == cache_chunks - 1 && sq.len % kPagePos : c == full;
+      return open ? sq.len % kPagePos : kChunk;
+    };
+    auto load = [&](int c, int page, int stage) {
+      const CT *k, *v;
+      long long step;
+      const int n = keys_of(c, page);
+      if (c >= cache_chunks) {
+        const long long at = ((long long)b * a.T + (c - cache_chunks) * kChunk) * a.kv_stride + tl.h * D;
+        k = reinterpret_cast<const CT*>(a.k_new) + at;
+        v = reinterpret_cast<const CT*>(a.v_new) + at;
+        step = a.kv_stride;
+      } else {
+        const long long at = ((long long)max(page, 0) * kPagePos * a.Hkv + tl.h) * D;
+        k = reinterpret_cast<const CT*>(a.k_pool) + at;
+        v = reinterpret_cast<const CT*>(a.v_pool) + at;
+        step = (long long)a.Hkv * D;
+      }
+      const uint32_t ks = ring_s + stage * L::STAGE, vs = ks + L::K_BYTES;
+      constexpr int PER_PASS = kThreads / L::PIECES >= 1 ? kThreads / L::PIECES : 1;
+      const int piece = tid % L::PIECES;
+#pragma unroll
+      for (int r0 = 0; r0 < kChunk; r0 += PER_PASS) {
+        const int r = r0 + tid / L::PIECES;
+        // rows behind the last key are filled with zeros: a weight of 0 times what lies there must be 0
+        const int bytes = r < n ? 16 : 0;
+        const long long at = r < n ? r * step + piece * L::PER : 0;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ks + L::k_at(r, piece)), "l"(k + at), "r"(bytes) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vs + L::v_at(r, piece)), "l"(v + at), "r"(bytes) : "memory");
+      }
+    };
+
+    // queries: bf16 fragments in registers, fp32 planes in shared memory
+    uint32_t qf[F32 ? 1 : KT][4];
+    if constexpr (F32) {
+      for (int i = tid; i < R * (D / 4); i += kThreads) {
+        const int r = i / (D / 4), c = i % (D / 4) * 4;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r < rows) x = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.q) + ((long long)b * a.T + node_of(r)) * a.q_stride + head_of(r) * D + c);
+        uint32_t p0[3], p1[3];
+        split3_pair(x.x, x.y, p0);
+        split3_pair(x.z, x.w, p1);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2*>(qs + (q * R + r) * S::QP + c) = make_uint2(p0[q], p1[q]);
+      }
+    } else {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int r = wr * 16 + g + half * 8;
+        const bf16* src = reinterpret_cast<const bf16*>(a.q);
+        if (r < rows) src += ((long long)b * a.T + node_of(r)) * a.q_stride + head_of(r) * D;
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+          qf[k][half] = r < rows ? *reinterpret_cast<const uint32_t*>(src + k * 16 + t4 * 2) : 0u;
+          qf[k][half + 2] = r < rows ? *reinterpret_cast<const uint32_t*>(src + k * 16 + t4 * 2 + 8) : 0u;
+        }
+      }
+    }
+    // the rows' lines in the tree, where the run reaches it
+    if (c_end > cache_chunks) {
+      if (lines_of != b) {
+        for (int i = tid; i < sq.nodes; i += kThreads) s_parents[i] = a.parents[(long long)b * a.T + i];
+        lines_of = b;
+      }
+      __syncthreads();
+      for (int i = tid; i < R * tree_chunks; i += kThreads) {
+        const int r = i % R, w = i / R;
+        s_line[r][w] = r < rows ? line_bits(s_parents, node_of(r), w) : 0ull;
+      }
+    }
+
+    float o[DT][4];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;   // maxima are of scores times scale_log2
+
+    // the ring: the number of keys of each chunk in it goes along (thread 0 writes, a barrier later all read)
+    int page_next = page_of(c_begin);                       // a table entry is fetched one chunk ahead of its rows
+#pragma unroll
+    for (int s = 0; s < S::STAGES - 1; ++s) {
+      const int c = c_begin + s;
+      if (c < c_end) {
+        load(c, page_next, s);
+        if (tid == 0) s_keys[s] = keys_of(c, page_next);
+        page_next = page_of(c + 1);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    int stage = 0;
+    for (int c = c_begin; c < c_end; ++c) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 2) : "memory");
+      __syncthreads();                                      // the chunk is there, and the stage before it has been used
+      {
+        const int cn = c + S::STAGES - 1, sn = stage == 0 ? S::STAGES - 1 : stage - 1;
+        if (cn < c_end) {
+          load(cn, page_next, sn);
+          if (tid == 0) s_keys[sn] = keys_of(cn, page_next);
+          page_next = page_of(cn + 1);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      }
+      const uint8_t* kb = ring + stage * L::STAGE;
+      const uint8_t* vb = kb + L::K_BYTES;
+      const uint32_t ks = ring_s + stage * L::STAGE, vs = ks + L::K_BYTES;
+      const int n_keys = s_keys[stage], key0 = wk * KW;
+
+      // scores of the warp's 16 rows and KW keys
+      float s[NT][4];
+#pragma unroll
+      for (int i = 0; i < NT; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+      if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          float lo[4] = {0.f, 0.f, 0.f, 0.f};               // the smaller products
+#pragma unroll 2
+          for (int k = 0; k < KT; ++k) {
+            const float* kr = reinterpret_cast<const float*>(kb) + (key0 + i * 8 + g) * L::KP + k * 16 + t4 * 2;
+            const float2 x = *reinterpret_cast<const float2*>(kr), y = *reinterpret_cast<const float2*>(kr + 8);
+            uint32_t b0[3], b1[3];
+            split3_pair(x.x, x.y, b0);
+            split3_pair(y.x, y.y, b1);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+              uint32_t aq[4];
+              ldsm4(s_addr(qs + (q * R + wr * 16 + (lane & 15)) * S::QP + k * 16 + (lane >> 4) * 8), aq);
+#pragma unroll
+              for (int p = 0; p < 3 - q; ++p) mma_bf16(p + q == 0 ? s[i] : lo, aq, b0[p], b1[p]);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[i][j] += lo[j];
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+#pragma unroll
+          for (int i = 0; i < NT; i += 2) {
+            uint32_t bk[4];
+            ldsm4(ks + L::swz(key0 + i * 8 + (lane & 7) + (lane >> 4) * 8, k * 2 + ((lane >> 3) & 1)), bk);
+            mma_bf16(s[i], qf[k], bk[0], bk[1]);
+            mma_bf16(s[i + 1], qf[k], bk[2], bk[3]);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i][j] *= a.scale_log2;
+
+      // what the rows do not see
+      if (c >= cache_chunks) {
+        const unsigned long long line0 = s_line[wr * 16 + g][c - cache_chunks], line1 = s_line[wr * 16 + g + 8][c - cache_chunks];
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int key = key0 + i * 8 + t4 * 2 + (j & 1);
+            if (!(((j < 2 ? line0 : line1) >> key) & 1)) s[i][j] = -INFINITY;
+          }
+      } else if (n_keys < kChunk) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) if (key0 + i * 8 + t4 * 2 + (j & 1) >= n_keys) s[i][j] = -INFINITY;
+      }
+
+      // running maximum and sum; weights
+      float n0 = m0, n1 = m1;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        n0 = fmaxf(n0, fmaxf(s[i][0], s[i][1]));
+        n1 = fmaxf(n1, fmaxf(s[i][2], s[i][3]));
+      }
+#pragma unroll
+      for (int off = 1; off < 4; off <<= 1) {
+        n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, off));
+        n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, off));
+      }
+      // (a row that has seen nothing keeps a maximum of -inf; its weights are taken against 0 and are 0)
+      const float base0 = n0 == -INFINITY ? 0.f : n0, base1 = n1 == -INFINITY ? 0.f : n1;
+      const float f0 = exp2f(m0 - base0), f1 = exp2f(m1 - base1);
+      m0 = n0; m1 = n1;
+      l0 *= f0; l1 *= f1;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        s[i][0] = exp2f(s[i][0] - base0); s[i][1] = exp2f(s[i][1] - base0);
+        s[i][2] = exp2f(s[i][2] - base1); s[i][3] = exp2f(s[i][3] - base1);
+        l0 += s[i][0] + s[i][1];
+        l1 += s[i][2] + s[i][3];
+      }
+
+      // A masked node's values may be infinite or not numbers, and 0 times those is not 0: where the tree's chunk holds
+      // such values, its products are taken one by one, without the keys whose weight is 0.
+      bool odd = false;
+      if (c >= cache_chunks) {
+        int bad = 0;
+        for (int i = tid; i < kChunk * D; i += kThreads) {
+          const int r = i / D, d = i % D;
+          float x;
+          if (F32) x = *reinterpret_cast<const float*>(vb + (r * L::VP + d) * 4);
+          else x = __bfloat162float(*reinterpret_cast<const bf16*>(vb + L::swz(r, d / 8) + (d % 8) * 2));
+          bad |= !(fabsf(x) <= 3.402823466e38f);
+        }
+        odd = __syncthreads_or(bad) != 0;
+      }
+      if (odd) {
+#pragma unroll
+        for (int n = 0; n < DT; ++n) { o[n][0] *= f0; o[n][1] *= f0; o[n][2] *= f1; o[n][3] *= f1; }
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk) {
+            const float w0 = __shfl_sync(0xffffffffu, s[i][kk & 1], (lane & ~3) | (kk >> 1));
+            const float w1 = __shfl_sync(0xffffffffu, s[i][2 + (kk & 1)], (lane & ~3) | (kk >> 1));
+            const int r = key0 + i * 8 + kk;
+#pragma unroll
+            for (int n = 0; n < DT; ++n)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const int d = n * 8 + t4 * 2 + e;
+                float x;
+                if (F32) x = *reinterpret_cast<const float*>(vb + (r * L::VP + d) * 4);
+                else x = __bfloat162float(*reinterpret_cast<const bf16*>(vb + L::swz(r, d / 8) + (d % 8) * 2));
+                if (w0 != 0.f) o[n][e] = fmaf(w0, x, o[n][e]);
+                if (w1 != 0.f) o[n][2 + e] = fmaf(w1, x, o[n][2 + e]);
+              }
+          }
+      } else if constexpr (F32) {
+#pragma unroll
+        for (int n = 0; n < DT; ++n) {
+          float acc[4] = {0.f, 0.f, 0.f, 0.f}, lo[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < NT / 2; ++k) {
+            const float* vr = reinterpret_cast<const float*>(vb) + (key0 + k * 16 + t4 * 2) * L::VP + n * 8 + g;
+            uint32_t b0[3], b1[3], w[4][3];
+            split3_pair(vr[0], vr[L::VP], b0);
+            split3_pair(vr[8 * L::VP], vr[9 * L::VP], b1);
+            split3_pair(s[2 * k][0], s[2 * k][1], w[0]);
+            split3_pair(s[2 * k][2], s[2 * k][3], w[1]);
+            split3_pair(s[2 * k + 1][0], s[2 * k + 1][1], w[2]);
+            split3_pair(s[2 * k + 1][2], s[2 * k + 1][3], w[3]);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+              const uint32_t ap[4] = {w[0][q], w[1][q], w[2][q], w[3][q]};
+#pragma unroll
+              for (int p = 0; p < 3 - q; ++p) mma_bf16(p + q == 0 ? acc : lo, ap, b0[p], b1[p]);
+            }
+          }
+          o[n][0] = fmaf(o[n][0], f0, acc[0] + lo[0]); o[n][1] = fmaf(o[n][1], f0, acc[1] + lo[1]);
+          o[n][2] = fmaf(o[n][2], f1, acc[2] + lo[2]); o[n][3] = fmaf(o[n][3], f1, acc[3] + lo[3]);
+        }
+      } else {
+#pragma unroll
+        for (int n = 0; n < DT; ++n) { o[n][0] *= f0; o[n][1] *= f0; o[n][2] *= f1; o[n][3] *= f1; }
+#pragma unroll
+        for (int k = 0; k < NT / 2; ++k) {
+          uint32_t hi[4], lo[4];
+          split2_pair(s[2 * k][0], s[2 * k][1], hi[0], lo[0]);
+          split2_pair(s[2 * k][2], s[2 * k][3], hi[1], lo[1]);
+          split2_pair(s[2 * k + 1][0], s[2 * k + 1][1], hi[2], lo[2]);
+          split2_pair(s[2 * k + 1][2], s[2 * k + 1][3], hi[3], lo[3]);
+#pragma unroll
+          for (int n = 0; n < DT; n += 2) {
+            uint32_t bv[4];
+            const uint32_t at = vs + L::swz(key0 + k * 16 + (lane & 15), n + (lane >> 4));
+            asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(bv[0]), "=r"(bv[1]), "=r"(bv[2]), "=r"(bv[3]) : "r"(at) : "memory");
+            mma_bf16(o[n], hi, bv[0], bv[1]);
+            mma_bf16(o[n + 1], hi, bv[2], bv[3]);
+            mma_bf16(o[n], lo, bv[0], bv[1]);
+            mma_bf16(o[n + 1], lo, bv[2], bv[3]);
+          }
+        }
+      }
+      stage = stage + 1 == S::STAGES ? 0 : stage + 1;
+    }
+
+    // join the warps that shared the rows
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();                                        // the ring has been used
+    l0 += __shfl_xor_sync(0xffffffffu, l0, 1); l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
+    l1 += __shfl_xor_sync(0xffffffffu, l1, 1); l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
+    float* mg = reinterpret_cast<float*>(ring);
+    if (t4 == 0) {
+      s_m[wk][wr * 16 + g] = m0; s_m[wk][wr * 16 + g + 8] = m1;
+      s_l[wk][wr * 16 + g] = l0; s_l[wk][wr * 16 + g + 8] = l1;
+    }
+#pragma unroll
+    for (int n = 0; n < DT; ++n) {
+      float* at = mg + (wk * R + wr * 16 + g) * S::MP + n * 8 + t4 * 2;
+      *reinterpret_cast<float2*>(at) = make_float2(o[n][0], o[n][1]);
+      *reinterpret_cast<float2*>(at + 8 * S::MP) = make_float2(o[n][2], o[n][3]);
+    }
+    __syncthreads();
+    const bool whole = c_begin == 0 && c_end == sq.w.chunks;
+    const int slot = u == u_begin ? 0 : 1;                  // a CTA leaves at most two partial results: of its first tile, of its last
+    float* part = a.part + ((long long)blockIdx.x * 2 + slot) * S::PART;
+    for (int i = tid; i < rows * (D / 4); i += kThreads) {
+      const int r = i / (D / 4), c4 = i % (D / 4) * 4;
+      float m = s_m[0][r];
+#pragma unroll
+      for (int w = 1; w < WK; ++w) m = fmaxf(m, s_m[w][r]);
+      const float base = m == -INFINITY ? 0.f : m;
+      float l = 0.f;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < WK; ++w) {
+        const float f = exp2f(s_m[w][r] - base);
+        const float4 y = *reinterpret_cast<const float4*>(mg + (w * R + r) * S::MP + c4);
+        l = fmaf(s_l[w][r], f, l);
+        if (f != 0.f) { x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w); }
+      }
+      if (whole) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const long long at = ((long long)b * a.T + node_of(r)) * a.H + head_of(r);
+        store4<CT>(reinterpret_cast<CT*>(a.out) + at * D + c4, make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv));
+        if (a.lse && c4 == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945f;
+      } else {
+        *reinterpret_cast<float4*>(part + r * D + c4) = x;
+        if (c4 == 0) { part[R * D + r] = m; part[R * D + R + r] = l; }
+      }
+    }
+    if (c_begin == 0 && tid == 0)
+      a.info[tl.id] = make_int2(blockIdx.x * 2 + slot, cta_of_unit(tile_first + sq.w.chunks - 1, units, ctas));
+    __syncthreads();                                        // the ring, the lines and the sums are free again
+    u = tile_first + c_end;
+  }
+}
+
+// Joins the partial results of the tiles that more than one CTA worked on.  grid: (tiles that could be, R / 4), a warp per row.
+template <typename CT, int D, int WR, bool PAGED>
+__global__ void __launch_bounds__(kThreads) combine_kernel(const __grid_constant__ AttnArgs a) {
+  using S = Shape<CT, D, WR>;
+  constexpr int R = S::R;
+  pdl_wait();                                               // (every CTA: the launch after this one waits for this one alone)
+  const int id = blockIdx.x, r = blockIdx.y * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  int b, h, t, r0;
+  if (PAGED) {
+    const int rt = ceil_div(a.G, R);
+    r0 = id % rt * R; h = id / rt % a.Hkv; t = id / rt / a.Hkv % a.T; b = id / rt / a.Hkv / a.T;
+  } else {
+    const int rt = ceil_div(a.T * a.G, R);
+    r0 = id % rt * R; h = id / rt % a.Hkv; b = id / rt / a.Hkv; t = 0;
+  }
+  const int nodes = a.nodes ? clamp_int(a.nodes[b], 0, a.T) : a.T;
+  const int rows = PAGED ? (t < nodes ? a.G : 0) : nodes * a.G;
+  if (r0 + r >= rows) return;
+  const int node = PAGED ? t : (r0 + r) / a.G, head = h * a.G + (PAGED ? r0 + r : (r0 + r) % a.G);
+  const int2 who = a.info[id];
+  if ((who.x >> 1) == who.y) return;
+  // a lane has 4 columns (D = 128), 2 (64) or 1
+  constexpr int E = D >= 64 ? D / 32 : 1;
+  const int col = lane * E;
+  float m = -INFINITY, l = 0.f, x[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = 0.f;
+  for (int c = who.x >> 1; c <= who.y; ++c) {
+    // all CTAs but the first begin their run inside the tile
+    const float* part = a.part + ((long long)c * 2 + (c == (who.x >> 1) ? (who.x & 1) : 0)) * S::PART;
+    const float pm = part[R * D + r], pl = part[R * D + R + r];
+    const float top = fmaxf(m, pm), base = top == -INFINITY ? 0.f : top;
+    const float f = exp2f(m - base), pf = exp2f(pm - base);
+    m = top;
+    l = l * f + pl * pf;
+    if (col < D) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) { const float y = part[r * D + col + e]; x[e] = x[e] * f + (pf != 0.f ? y * pf : 0.f); }
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const long long at = ((long long)b * a.T + node) * a.H + head;
+  if (col < D) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) reinterpret_cast<CT*>(a.out)[at * D + col + e] = from_f<CT>(x[e] * inv);
+  }
+  if (a.lse && lane == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945f;
+}
+
+}  // namespace tree
+}  // namespace bpd

@@ -1,0 +1,76 @@
+// Launches of the tree attention kernels, per element type (one translation unit each).
+#pragma once
+#include "host.hpp"
+#include "tree_attention.cuh"
+
+namespace bpd {
+namespace tree {
+
+constexpr int kSMs = 148;
+
+// What a call of these sizes needs, and its launches.
+struct AttnPlan {
+  int ctas, tile_rows, tiles, combine_rows;   // tiles: that could be
+  size_t part_bytes, info_bytes;
+};
+// Rows of a tile: as few as hold all rows of a key head, 64 at most.
+inline int tile_rows_of(bool paged, int rows) { return paged || rows <= 16 ? 16 : (rows <= 32 ? 32 : 64); }
+
+template <typename CT> int plan_attention(const AttnArgs& a, bool paged, int D, AttnPlan* plan);
+template <typename CT> int launch_attention(const AttnArgs& a, bool paged, int D, const AttnPlan& plan, cudaStream_t st);
+
+template <typename CT, int D, int WR, bool PAGED>
+int plan_one(const AttnArgs& a, AttnPlan* p) {
+  using S = Shape<CT, D, WR>;
+  p->tile_rows = S::R;
+  const long long per_head = PAGED ? ceil_div(a.G, S::R) : ceil_div(a.T * a.G, S::R);
+  const long long tiles = (long long)a.B * a.Hkv * per_head * (PAGED ? a.T : 1);
+  if (tiles > 0x7fffffffLL) return fail(BPD_E_SHAPE, "batch * nodes * heads out of range");
+  p->tiles = (int)tiles;
+  const long long chunks = (PAGED ? std::min(a.select, a.ppr) + 1 : a.ppr) + ceil_div(a.T, kChunk);
+  p->ctas = (int)std::min<long long>(tiles * chunks, (long long)kSMs * S::CTAS_PER_SM);
+  p->combine_rows = std::min(S::R, PAGED ? a.G : a.T * a.G);
+  p->part_bytes = (((size_t)p->ctas * 2 * S::PART * 4) + 255) / 256 * 256;
+  p->info_bytes = ((size_t)p->tiles * sizeof(int2) + 255) / 256 * 256;
+  return BPD_OK;
+}
+
+template <typename CT, int D, int WR, bool PAGED>
+int launch_one(const AttnArgs& a, const AttnPlan& p, cudaStream_t st) {
+  using S = Shape<CT, D, WR>;
+  int rc = ensure_smem_limit(reinterpret_cast<const void*>(tree_attention_kernel<CT, D, WR, PAGED>), S::SMEM);
+  if (rc) return rc;
+  BPD_CUDA(launch_k(tree_attention_kernel<CT, D, WR, PAGED>, dim3(p.ctas), dim3(kThreads), S::SMEM, st, false, a));
+  BPD_CUDA(launch_k(combine_kernel<CT, D, WR, PAGED>, dim3(p.tiles, ceil_div(p.combine_rows, 4)), dim3(kThreads), 0, st, true, a));
+  g_launches += 2;
+  return BPD_OK;
+}
+
+template <typename CT, int D, typename F>
+int by_rows(const AttnArgs& a, bool paged, F&& f) {
+  if (paged) return f(std::integral_constant<int, 1>(), std::true_type());
+  switch (tile_rows_of(false, a.T * a.G)) {
+    case 16: return f(std::integral_constant<int, 1>(), std::false_type());
+    case 32: return f(std::integral_constant<int, 2>(), std::false_type());
+    default: return f(std::integral_constant<int, 4>(), std::false_type());
+  }
+}
+
+#define BPD_TREE_BY_DIM(call)                \
+  switch (D) {                               \
+    case 16: { constexpr int DD = 16; call } \
+    case 32: { constexpr int DD = 32; call } \
+    case 64: { constexpr int DD = 64; call } \
+    default: { constexpr int DD = 128; call }\
+  }
+
+#define BPD_TREE_INSTANTIATE(CT)                                                                          \
+  template <> int plan_attention<CT>(const AttnArgs& a, bool paged, int D, AttnPlan* plan) {              \
+    BPD_TREE_BY_DIM(return (by_rows<CT, DD>(a, paged, [&](auto wr, auto pg) { return plan_one<CT, DD, decltype(wr)::value, decltype(pg)::value>(a, plan); }));) \
+  }                                                                                                       \
+  template <> int launch_attention<CT>(const AttnArgs& a, bool paged, int D, const AttnPlan& plan, cudaStream_t st) { \
+    BPD_TREE_BY_DIM(return (by_rows<CT, DD>(a, paged, [&](auto wr, auto pg) { return launch_one<CT, DD, decltype(wr)::value, decltype(pg)::value>(a, plan, st); }));) \
+  }
+
+}  // namespace tree
+}  // namespace bpd

@@ -1,0 +1,369 @@
+"""The operators on a paged cache against their definitions in 64 bits (oracle/operators.py), at the sizes, layouts and
+contents where they can go wrong.  Whatever no call may read -- positions behind a sequence's length, pages nobody owns --
+holds NaN."""
+import numpy as np
+import pytest
+
+from oracle import operators as plain
+
+pytestmark = pytest.mark.gpu
+PAGE = 64
+
+
+@pytest.fixture(scope="module")
+def bpd():
+    import paper_1811_03115_b200 as b
+    return b
+
+
+def _round(x, dtype):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(x, np.float32))
+    return t.bfloat16().float().numpy() if dtype == "bf16" else t.numpy()
+
+
+def _dev(x, dtype=None):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(x))
+    return t.to("cuda", torch.bfloat16 if dtype == "bf16" else t.dtype)
+
+
+class Case:
+    """A cache of ``layers`` layers with NaN wherever nothing was written, drafted nodes and their trees."""
+
+    def __init__(self, seed, lens, nodes, heads, kv_heads, dim, dtype, layers=1, tree="random", live=None, spare=1):
+        rng = self.rng = np.random.default_rng(seed)
+        b = len(lens)
+        self.lens, self.heads, self.kv_heads, self.dim, self.dtype, self.layers = np.asarray(lens, np.int32), heads, kv_heads, dim, dtype, layers
+        ppr = max(1, -(-(int(max(lens)) + nodes) // PAGE))
+        n_pages = b * ppr + spare
+        self.table = rng.permutation(n_pages)[:b * ppr].reshape(b, ppr).astype(np.int32)
+        shape = (layers, n_pages, PAGE, kv_heads, dim)
+        self.k, self.v = np.full(shape, np.nan, np.float32), np.full(shape, np.nan, np.float32)
+        for r, n in enumerate(lens):
+            s = np.arange(n)
+            for pool in (self.k, self.v):
+                pool[:, self.table[r, s // PAGE], s % PAGE] = _round(rng.standard_normal((layers, n, kv_heads, dim)), dtype)
+        self.q = _round(1.5 * rng.standard_normal((b, nodes, heads, dim)), dtype)
+        self.k_new, self.v_new = (_round(rng.standard_normal((layers, b, nodes, kv_heads, dim)), dtype) for _ in range(2))
+        t = np.arange(nodes)
+        if tree == "chain":
+            self.parents = np.tile(t - 1, (b, 1)).astype(np.int32)
+        elif tree == "star":
+            self.parents = np.full((b, nodes), -1, np.int32)
+        else:
+            self.parents = np.stack([np.maximum(t - 1 - rng.integers(0, 4, nodes), -1) for _ in range(b)]).astype(np.int32)
+        self.nodes = np.full(b, nodes, np.int32) if live is None else np.asarray(live, np.int32)
+        self.scale = dim ** -0.5
+
+    def pools(self, layer=None):
+        k, v = (self.k, self.v) if layer is None else (self.k[layer], self.v[layer])
+        return _dev(k, self.dtype), _dev(v, self.dtype), _dev(self.table)
+
+    def drafted(self, layer=0):
+        return _dev(self.q, self.dtype), _dev(self.k_new[layer], self.dtype), _dev(self.v_new[layer], self.dtype)
+
+    def weight_error(self):
+        """Bound on the relative error of a softmax weight: the scores' (every step of 16 products may lose 2^-23 of the partial
+        sum, which is at most sum |q||k|; the scale's rounding; log2(e) goes into it), the exponential's 2 units, the weight's
+        16 (bf16) or 24 (fp32) bits, and the sum's, which is added up chunk by chunk."""
+        keys = np.abs(np.nan_to_num(np.concatenate([self.k.reshape(-1, self.dim), self.k_new.reshape(-1, self.dim)], 0), posinf=0., neginf=0.)).max()
+        score = self.scale * float(np.abs(np.nan_to_num(self.q, posinf=0., neginf=0.)).sum(-1).max()) * float(keys)
+        chunks = max(self.lens) / 64 + 8
+        return score * (self.dim / 16 + 4) * 2.0 ** -23, 2.0 ** -21 + (2.0 ** -17 if self.dtype == "bf16" else 2.0 ** -22) + 4 * chunks * 2.0 ** -24
+
+    def check(self, got, want, want_lse, lse):
+        score, rest = self.weight_error()
+        far = np.nanmax(np.abs(want)) if want.size else 1.0
+        # weights and their sum are both off by `score` and `rest`; values are below max |v|
+        top = np.nanmax(np.abs(np.nan_to_num(np.concatenate([self.v.reshape(-1), self.v_new.reshape(-1)]), posinf=0., neginf=0.)))
+        half = 2.0 ** -8 if self.dtype == "bf16" else 2.0 ** -23
+        tol = 2 * (score + rest) * max(top, far) + half * np.abs(want)
+        got = got.double().cpu().numpy()
+        assert got.shape == want.shape and not np.isnan(got).any()
+        assert (np.abs(got - want) <= tol).all(), float((np.abs(got - want) - tol).max())
+        if lse is not None:
+            lse = lse.double().cpu().numpy()
+            assert np.array_equal(np.isinf(lse), np.isinf(want_lse)) and (lse[np.isinf(lse)] < 0).all()
+            seen = ~np.isinf(want_lse)
+            assert (np.abs(lse - want_lse)[seen] <= (score + rest + 2.0 ** -22 * np.abs(want_lse[seen]) + 2.0 ** -21)).all()
+
+
+# lengths 0 and 1, page edges, tiles of 16, 32 and 64 rows and several of them, groups that do not divide a tile, trees that
+# span several words, rows with fewer nodes than others and with none
+TREES = [
+    ([0], 1, 1, 1, 16, "chain", None), ([1], 1, 4, 4, 64, "chain", None), ([63, 64, 65], 1, 8, 2, 128, "chain", None),
+    ([130, 0, 200], 10, 4, 4, 64, "chain", [10, 3, 0]), ([100, 7], 13, 6, 2, 32, "random", [13, 5]), ([1000], 5, 24, 2, 64, "random", None),
+    ([300, 64], 33, 2, 2, 128, "random", [33, 1]), ([700, 5], 64, 4, 2, 64, "random", [64, 50]), ([90], 65, 3, 1, 16, "random", None),
+    ([129], 200, 2, 1, 64, "random", None), ([20], 256, 1, 1, 32, "chain", None), ([64], 100, 2, 2, 128, "star", None),
+    ([2500, 1, 640, 64], 3, 16, 1, 128, "random", [3, 1, 2, 3]), ([40] * 130, 2, 2, 1, 16, "chain", None),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens,nodes,heads,kv_heads,dim,tree,live", TREES)
+def test_tree_attention(bpd, lens, nodes, heads, kv_heads, dim, tree, live, dtype):
+    c = Case(nodes * dim + len(lens), lens, nodes, heads, kv_heads, dim, dtype, tree=tree, live=live)
+    want, want_lse = plain.attention(c.q, c.k_new[0], c.v_new[0], c.k[0], c.v[0], c.table, c.lens, c.parents, c.nodes, c.scale)
+    out, lse = bpd.bpd_op_tree_attention(*c.drafted(), *c.pools(0), _dev(c.lens), _dev(c.parents), None if live is None else _dev(c.nodes), want_lse=True)
+    c.check(out, want, want_lse, lse)
+    again = bpd.bpd_op_tree_attention(*c.drafted(), *c.pools(0), _dev(c.lens), _dev(c.parents), None if live is None else _dev(c.nodes))
+    assert bool((again == out).all())                       # the same call gives the same bits
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_tree_attention_of_slices_of_one_projection(bpd, dtype):
+    import torch
+    c = Case(3, [70, 130], 5, 4, 2, 64, dtype)
+    width = (4 + 2 * 2) * 64
+    fused = torch.full((2, 5, width + 16), float("nan"), device="cuda", dtype=_dev(c.q, dtype).dtype)
+    q, k, v = c.drafted()
+    fused[..., :256], fused[..., 256:384], fused[..., 384:512] = q.flatten(2), k.flatten(2), v.flatten(2)
+    parts = fused[..., :256].unflatten(2, (4, 64)), fused[..., 256:384].unflatten(2, (2, 64)), fused[..., 384:512].unflatten(2, (2, 64))
+    got = bpd.bpd_op_tree_attention(*parts, *c.pools(0), _dev(c.lens), _dev(c.parents), scale=0.3)
+    assert bool((got == bpd.bpd_op_tree_attention(q, k, v, *c.pools(0), _dev(c.lens), _dev(c.parents), scale=0.3)).all())
+    c.scale = 0.3
+    c.check(got, *plain.attention(c.q, c.k_new[0], c.v_new[0], c.k[0], c.v[0], c.table, c.lens, c.parents, c.nodes, 0.3), None)
+
+
+# siblings hold infinities and NaN: only their own lines may see them
+@pytest.mark.parametrize("dtype,dim,nodes", [("bf16", 64, 9), ("fp32", 64, 9), ("bf16", 128, 40), ("fp32", 16, 20)])
+def test_values_that_are_no_numbers_stay_in_their_line(bpd, dtype, dim, nodes):
+    c = Case(5, [10, 0], nodes, 2, 1, dim, dtype, tree="star")
+    c.parents[:, 3] = 1
+    c.parents[:, 4] = 3
+    bad = [2, 5, nodes - 1]
+    c.k_new[:, :, 2], c.v_new[:, :, 2] = np.nan, np.inf
+    c.v_new[:, :, 5, :, ::3] = np.nan
+    c.k_new[:, :, nodes - 1], c.v_new[:, :, nodes - 1, :, 1] = np.inf, -np.inf
+    want, want_lse = plain.attention(c.q, c.k_new[0], c.v_new[0], c.k[0], c.v[0], c.table, c.lens, c.parents, c.nodes, c.scale)
+    out, lse = bpd.bpd_op_tree_attention(*c.drafted(), *c.pools(0), _dev(c.lens), _dev(c.parents), want_lse=True)
+    fine = [t for t in range(nodes) if t not in bad]
+    c.check(out[:, fine], want[:, fine], want_lse[:, fine], lse[:, fine])
+    assert bool(out[:, 2].isnan().all()) and bool(out[:, 5, :, ::3].isnan().all()) and bool(out[:, 5, :, 1::3].isfinite().all())
+
+
+# pages outside the pool, parents that do not lie before their node, lengths and node counts outside their ranges
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_values_of_device_arrays_are_not_trusted(bpd, dtype):
+    c = Case(6, [200, 130, 90], 6, 4, 2, 32, dtype, spare=3)
+    c.table[0, 1], c.table[1, 2], c.table[2, 0] = -1, len(c.k[0]), 2 ** 31 - 1
+    c.parents[0] = [5, 1, 7, -3, 2, 2]
+    out, lse = bpd.bpd_op_tree_attention(*c.drafted(), *c.pools(0), _dev(c.lens), _dev(c.parents), want_lse=True)
+    c.check(out, *plain.attention(c.q, c.k_new[0], c.v_new[0], c.k[0], c.v[0], c.table, c.lens, c.parents, c.nodes, c.scale), lse)
+    lens, nodes = np.array([-5, 2 ** 31 - 1, 90], np.int32), np.array([99, -2, 2 ** 31 - 1], np.int32)
+    c.k[:], c.v[:] = np.nan_to_num(c.k), np.nan_to_num(c.v)
+    out, lse = bpd.bpd_op_tree_attention(*c.drafted(), *c.pools(0), _dev(lens), _dev(c.parents), _dev(nodes), want_lse=True)
+    c.nodes, c.lens = np.array([6, 0, 6], np.int32), np.array([0, 256, 90], np.int32)
+    c.check(out, *plain.attention(c.q, c.k_new[0], c.v_new[0], c.k[0], c.v[0], c.table, c.lens, c.parents, c.nodes, c.scale), lse)
+
+
+PAGED = [
+    ([0], 1, 1, 1, 16, 1, None), ([64], 1, 2, 2, 64, 1, None), ([63], 2, 4, 2, 64, 3, None), ([1000, 130], 3, 8, 2, 128, 4, [3, 2]),
+    ([700, 64, 65, 5], 2, 20, 1, 64, 5, [2, 0, 1, 2]), ([2000], 1, 40, 2, 32, 7, None), ([5000], 4, 4, 4, 16, 30, None), ([640], 70, 2, 1, 64, 2, [70]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens,nodes,heads,kv_heads,dim,select,live", PAGED)
+def test_page_attention(bpd, lens, nodes, heads, kv_heads, dim, select, live, dtype):
+    import torch
+    c = Case(nodes + dim + len(lens), lens, nodes, heads, kv_heads, dim, dtype, live=live)
+    means = plain.page_means(c.k[0], c.table, c.lens)
+    k, v, table = c.pools(0)
+    held = torch.full((1,) + means.shape, float("nan"), device="cuda")
+    half = np.maximum(c.lens // 2, 0).astype(np.int32)
+    bpd.bpd_op_page_means(k[None], table, _dev(np.zeros_like(half)), _dev(half), held)          # in two steps, as a cache grows
+    bpd.bpd_op_page_means(k[None], table, _dev(half), _dev(c.lens), held)
+    got = held[0].cpu().numpy()
+    assert np.array_equal(np.isnan(got), np.isnan(means))
+    np.testing.assert_allclose(np.nan_to_num(got), np.nan_to_num(means), rtol=2.0 ** -23)
+    means = got
+    want, want_lse, pages = plain.page_attention(c.q, c.k_new[0], c.v_new[0], c.k[0], c.v[0], c.table, means, c.lens, c.parents, select, c.nodes, c.scale)
+    out, lse, chosen = bpd.bpd_op_page_attention(*c.drafted(), k, v, table, held[0], _dev(c.lens), _dev(c.parents), select,
+                                                 None if live is None else _dev(c.nodes), want_lse=True, want_pages=True)
+    assert np.array_equal(chosen.cpu().numpy(), pages)
+    c.check(out, want, want_lse, lse)
+
+
+def test_page_selection_orders_ties_and_no_numbers(bpd):
+    c = Case(9, [64 * 9 + 3], 1, 2, 1, 64, "fp32")
+    means = np.zeros((1, 10, 1, 64), np.float32)
+    means[0, :9, 0, 0] = [1, 2, np.nan, 2, -np.inf, 2, 0, -0.0, 2]
+    c.q[:] = 0
+    c.q[0, 0, :, 0] = [0.25, 0.75]
+    for select, want in ((2, [1, 3]), (5, [0, 1, 3, 5, 8]), (7, [0, 1, 3, 5, 6, 7, 8])):
+        # a product of 0 and -inf is no number either: page 4's scores are NaN where the query is 0, and go with page 2
+        pages = bpd.bpd_op_page_attention(*c.drafted(), *c.pools(0), _dev(means), _dev(c.lens), _dev(c.parents), select, want_pages=True)[1]
+        assert pages[0, 0, 0].tolist() == want
+    assert bpd.bpd_op_page_attention(*c.drafted(), *c.pools(0), _dev(means), _dev(c.lens), _dev(c.parents), 8, want_pages=True)[1][0, 0, 0].tolist() == [0, 1, 3, 4, 5, 6, 7, 8]
+    assert bpd.bpd_op_page_attention(*c.drafted(), *c.pools(0), _dev(means), _dev(c.lens), _dev(c.parents), 12, want_pages=True)[1][0, 0, 0].tolist() == list(range(9)) + [-1] * 3
+
+
+@pytest.mark.parametrize("layers,lens,nodes,kv_heads,dim,dtype,eos", [(1, [0], 1, 1, 16, "bf16", -1), (3, [62, 5, 127], 9, 2, 64, "fp32", -1),
+                                                                      (2, [60] * 40, 33, 4, 32, "bf16", 1), (6, [10, 128], 256, 8, 128, "bf16", -1)])
+def test_tree_commit(bpd, layers, lens, nodes, kv_heads, dim, dtype, eos):
+    b = len(lens)
+    c = Case(layers * nodes, lens, nodes, kv_heads, kv_heads, dim, dtype, layers=layers, live=None if nodes == 1 else [nodes - (r % 3) for r in range(b)])
+    tokens, top1, last = (c.rng.integers(0, 2, s).astype(np.int32) for s in ((b, nodes), (b, nodes), b))
+    tokens[0], top1[0], last[0] = 0, 0, 0                    # a long walk
+    want = plain.commit(c.k_new, c.v_new, c.k, c.v, c.table, c.lens, c.parents, tokens, top1, last, c.nodes, eos)
+    k, v, table = c.pools()
+    got = bpd.bpd_op_tree_commit(_dev(c.k_new, dtype), _dev(c.v_new, dtype), k, v, table, _dev(c.lens), _dev(c.parents), _dev(tokens), _dev(top1), _dev(last),
+                                 _dev(c.nodes), eos_id=eos)
+    for x, y in zip(got + (k, v), want):
+        assert np.array_equal(x.float().cpu().numpy(), np.asarray(y, np.float32), equal_nan=True)
+
+
+def test_tree_commit_stops_where_the_cache_is_full(bpd):
+    c = Case(4, [125, 128, 120], 8, 1, 1, 16, "fp32", tree="chain")
+    c.table = c.table[:, :2].copy()
+    c.table[2, 1] = -1                                       # that row's second page is missing: its entries are not written
+    zeros = np.zeros((3, 8), np.int32)
+    k, v, table = c.pools()
+    got = bpd.bpd_op_tree_commit(_dev(c.k_new), _dev(c.v_new), k, v, table, _dev(c.lens), _dev(c.parents), _dev(zeros), _dev(zeros), _dev(zeros[:, 0]))
+    assert got[0].tolist() == [128, 128, 128] and got[1].tolist() == [3, 0, 8]
+    want = plain.commit(c.k_new, c.v_new, c.k, c.v, c.table, c.lens, c.parents, zeros, zeros, zeros[:, 0], c.nodes)
+    assert np.array_equal(k.cpu().numpy(), want[4], equal_nan=True) and np.array_equal(v.cpu().numpy(), want[5], equal_nan=True)
+    bad = bpd.bpd_op_tree_commit(_dev(c.k_new), _dev(c.v_new), k, v, table, _dev(np.array([-1, 129, 128], np.int32)), _dev(c.parents), _dev(zeros), _dev(zeros),
+                                 _dev(zeros[:, 0]))
+    assert bad[1].tolist() == [0, 0, 0] and np.array_equal(k.cpu().numpy(), want[4], equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens,nodes,heads,kv_heads,dim", [([0], 1, 1, 1, 16), ([63, 64, 1], 3, 4, 2, 64), ([600, 0, 1100], 5, 8, 2, 128), ([130], 40, 6, 2, 32),
+                                                           ([513], 20, 16, 2, 16)])
+def test_cache_weights(bpd, lens, nodes, heads, kv_heads, dim, dtype):
+    c = Case(dim + nodes, lens, nodes, heads, kv_heads, dim, dtype, tree="chain")
+    b, cap = len(lens), c.table.shape[1] * PAGE
+    accepted = np.array([min(nodes, 1 + 2 * r + nodes // 2) for r in range(b)], np.int32)
+    if b > 2:
+        accepted[2] = 0
+    # the path's nodes in ascending order, their keys in the cache as the commit leaves them
+    path = np.full((b, nodes), -1, np.int32)
+    for r in range(b):
+        path[r, :accepted[r]] = np.sort(c.rng.permutation(nodes)[:accepted[r]])
+        for i in range(accepted[r]):
+            s = lens[r] + i
+            c.k[0, c.table[r, s // PAGE], s % PAGE] = c.k_new[0, r, path[r, i]]
+    lse = np.full((b, nodes, heads), np.nan, np.float32)
+    for r in range(b):
+        for i in range(accepted[r]):
+            for g in range(heads):
+                keys = plain.cached(c.k[0][:, :, g * kv_heads // heads], c.table[r], range(lens[r] + i + 1))
+                lse[r, path[r, i], g] = plain.softmax_row(c.q[r, path[r, i], g].astype(np.float64), keys, keys, c.scale)[1]
+    weights = c.rng.random((b, kv_heads, cap)).astype(np.float32)
+    positions = c.rng.integers(0, 1000, (b, kv_heads, cap)).astype(np.int32)
+    seen = np.arange(b).astype(np.int32) * 1000 + 7
+    want_w, want_p = plain.cache_weights(c.q, lse, path, accepted, c.k[0], c.table, c.lens, seen, weights, positions, c.scale)
+    k, _, table = c.pools(0)
+    got_w, got_p = _dev(weights), _dev(positions)
+    bpd.bpd_op_cache_weights(_dev(c.q, dtype), _dev(lse), _dev(path), _dev(accepted), k, table, _dev(c.lens), _dev(seen), got_w, got_p)
+    assert np.array_equal(got_p.cpu().numpy(), want_p)
+    score, _ = c.weight_error()
+    # a weight's exponent is off by the score's error, and by the rounding of the difference to lse; the exponential by 2 units, the
+    # sums by one rounding for each of up to 64 rows
+    off = score + 2.0 ** -24 * np.nanmax(np.abs(lse)) + 2.0 ** -21 + 64 * 2.0 ** -24
+    got = got_w.double().cpu().numpy()
+    assert (np.abs(got - want_w) <= off * (want_w + 1e-30) + 2.0 ** -23 * want_w).all()
+    untouched = np.ones_like(weights, bool)
+    for r in range(b):
+        untouched[r, :, :lens[r] + accepted[r] if accepted[r] else 0] = False
+    assert np.array_equal(got_w.cpu().numpy()[untouched], weights[untouched])
+
+
+EVICT = [(1, [1], 1, 16, 1, 0, "bf16"), (2, [65, 10, 64], 2, 32, 20, 5, "fp32"), (1, [522], 4, 64, 512, 64, "fp32"), (3, [700, 300], 2, 128, 100, 100, "bf16"),
+         (1, [1500, 1], 3, 64, 1, 0, "bf16"), (2, [3000], 2, 16, 2999, 7, "bf16"), (1, [1024, 513, 512], 1, 32, 512, 0, "fp32")]
+
+
+@pytest.mark.parametrize("kind", ["random", "ties", "odd"])
+@pytest.mark.parametrize("layers,lens,kv_heads,dim,budget,recent,dtype", EVICT)
+def test_cache_evict(bpd, layers, lens, kv_heads, dim, budget, recent, dtype, kind):
+    c = Case(budget + dim, lens, 1, kv_heads, kv_heads, dim, dtype, layers=layers)
+    b, cap = len(lens), c.table.shape[1] * PAGE
+    shape = (layers, b, kv_heads, cap)
+    weights = c.rng.random(shape).astype(np.float32)
+    if kind == "ties":
+        weights = np.floor(weights * 3).astype(np.float32) - 1                  # -1, 0, 1
+        weights[..., ::5] = -0.0
+    elif kind == "odd":
+        weights[c.rng.random(shape) < 0.3] = np.nan
+        weights[c.rng.random(shape) < 0.1] = -np.inf
+        weights[c.rng.random(shape) < 0.1] = np.inf
+    positions = np.stack([c.rng.permutation(cap) for _ in range(layers * b * kv_heads)]).reshape(shape).astype(np.int32)
+    seen = np.array([cap - 3 * r for r in range(b)], np.int32)
+    want = plain.evict(weights, positions, c.k, c.v, c.table, c.lens, seen, budget, recent)
+    k, v, table = c.pools()
+    w, p = _dev(weights), _dev(positions)
+    got = bpd.bpd_op_cache_evict(w, p, k, v, table, _dev(c.lens), _dev(seen), budget, recent)
+    for x, y in zip((got, w, p, k, v), want):
+        assert np.array_equal(x.float().cpu().numpy(), np.asarray(y, np.float32), equal_nan=True)
+
+
+# a program's step: attention over the cache and the tree, commit, weights, eviction, and the next step's attention over what is
+# left, eagerly and as one captured graph replayed on another stream
+def _steps(bpd, c, state, budget):
+    out, lse = bpd.bpd_op_tree_attention(state["q"], state["k_new"][0], state["v_new"][0], state["k"][0], state["v"][0], state["table"], state["lens"],
+                                         state["parents"], want_lse=True)
+    lens, accepted, path, following = bpd.bpd_op_tree_commit(state["k_new"], state["v_new"], state["k"], state["v"], state["table"], state["lens"],
+                                                             state["parents"], state["tokens"], state["top1"], state["last"])
+    bpd.bpd_op_cache_weights(state["q"], lse, path, accepted, state["k"][0], state["table"], state["lens"], state["seen"], state["weights"][0],
+                             state["positions"][0])
+    left = bpd.bpd_op_cache_evict(state["weights"], state["positions"], state["k"], state["v"], state["table"], lens, state["seen"] + accepted, budget, 8)
+    after, _ = bpd.bpd_op_tree_attention(state["q"], state["k_new"][0], state["v_new"][0], state["k"][0], state["v"][0], state["table"], left, state["parents"],
+                                         want_lse=True)
+    state["means"].zero_()
+    bpd.bpd_op_page_means(state["k"], state["table"], state["zero"], left, state["means"])
+    paged, pages = bpd.bpd_op_page_attention(state["q"], state["k_new"][0], state["v_new"][0], state["k"][0], state["v"][0], state["table"], state["means"][0],
+                                             left, state["parents"], 1, want_pages=True)
+    return out, lse, lens, accepted, path, following, left, after, paged, pages
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_a_step_of_all_operators(bpd, captured):
+    import torch
+    budget = 130
+    c = Case(11, [150, 131, 40], 7, 4, 2, 64, "fp32", live=None)
+    b, cap = 3, c.table.shape[1] * PAGE
+    tokens, top1, last = np.zeros((b, 7), np.int32), np.zeros((b, 7), np.int32), np.zeros(b, np.int32)
+    weights, seen = c.rng.random((1, b, 2, cap)).astype(np.float32), c.lens.copy()
+    positions = np.broadcast_to(np.arange(cap, dtype=np.int32), (1, b, 2, cap)).copy()
+    host = {"k_new": c.k_new, "v_new": c.v_new, "k": c.k, "v": c.v, "table": c.table, "lens": c.lens, "parents": c.parents, "tokens": tokens, "top1": top1,
+            "last": last, "weights": weights, "positions": positions, "seen": seen, "q": c.q, "zero": np.zeros(b, np.int32),
+            "means": np.zeros((1,) + c.table.shape + (2, 64), np.float32)}
+    state = {n: _dev(x) for n, x in host.items()}
+    if captured:
+        stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        with torch.cuda.stream(stream):
+            _steps(bpd, c, state, budget)                  # loads the kernels
+            with torch.cuda.graph(graph, stream=stream):
+                got = _steps(bpd, c, state, budget)
+        torch.cuda.synchronize()
+        for n, x in host.items():
+            state[n].copy_(torch.from_numpy(x))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(torch.cuda.Stream()):
+            graph.replay()
+        torch.cuda.synchronize()
+    else:
+        got = _steps(bpd, c, state, budget)
+    out, lse, lens, accepted, path, following, left, after, paged, pages = got
+    want, want_lse = plain.attention(c.q, c.k_new[0], c.v_new[0], c.k[0], c.v[0], c.table, c.lens, c.parents, c.nodes, c.scale)
+    c.check(out, want, want_lse, lse)
+    new = plain.commit(c.k_new, c.v_new, c.k, c.v, c.table, c.lens, c.parents, tokens, top1, last, c.nodes)
+    for x, y in zip((lens, accepted, path, following), new):
+        assert np.array_equal(x.cpu().numpy(), y)
+    assert accepted.min() >= 1
+    k, v = new[4], new[5]
+    w, p = plain.cache_weights(c.q, want_lse, new[2], new[1], k[0], c.table, c.lens, seen, weights[0], positions[0], c.scale)
+    # the library's weights are these to rounding; drawn weights lie far enough apart that the same entries stay
+    lefts, w, p, k, v = plain.evict(w[None], p[None], k, v, c.table, new[0], seen + new[1], budget, 8)
+    assert np.array_equal(left.cpu().numpy(), lefts) and lefts.tolist()[:2] == [130, 130]
+    assert np.array_equal(state["positions"].cpu().numpy(), p)
+    assert np.array_equal(state["k"].cpu().numpy(), k, equal_nan=True) and np.array_equal(state["v"].cpu().numpy(), v, equal_nan=True)
+    c.k, c.v, c.lens = k, v, lefts
+    c.check(after, *plain.attention(c.q, c.k_new[0], c.v_new[0], k[0], v[0], c.table, lefts, c.parents, c.nodes, c.scale), None)
+    means = state["means"][0].cpu().numpy()
+    far = plain.page_attention(c.q, c.k_new[0], c.v_new[0], k[0], v[0], c.table, means, lefts, c.parents, 1, c.nodes, c.scale)
+    assert np.array_equal(pages.cpu().numpy(), far[2])
+    c.check(paged, far[0], far[1], None)
