@@ -12,6 +12,7 @@ from dataclasses import dataclass
 from typing import Optional
 
 import numpy as np
+import torch
 
 from .build import LIB_PATH
 
@@ -406,20 +407,23 @@ def bpd_op_linear(x, w, bias=None, relu: bool = False):
 # ---------------------------------------------------------------------- operators on a paged cache
 # Shapes: pools [layers, pages, 64, kv_heads, head_dim] (one layer's: without the first), page_table int32 [batch,
 # pages_per_row], drafted nodes [batch, nodes, heads, head_dim].  float32 or bfloat16 throughout.  All calls enqueue on the
-# current stream of the tensors' device and may be captured.
+# current stream of the tensors' device and may be captured.  The smallest of them take less time on the device than their
+# checks do here, so these are written for speed: the index of a tensor's device instead of the device, one constructor call
+# for the structure, no context manager where the device is current already, sizes of new tensors as separate arguments (a
+# tuple takes torch twice the time).
 
 def _expect(t, name, shape, dtype, device):
-    """A contiguous tensor of this shape, type and device."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} "
-                         f"{tuple(t.shape)} on {t.device}")
+    """Address of a contiguous tensor of this shape and type on the device of this index."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on device {device}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
     return t.data_ptr()
 
 
 def _expect_rows(t, name, shape, dtype, device):
-    """A tensor whose last two dimensions are contiguous and whose rows before them are one stride apart.  Returns address, stride."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} "
+    """Address and row stride of a tensor whose last two dimensions are contiguous and whose rows before them are one stride apart."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        raise ValueError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on device {device}, got {t.dtype} {tuple(t.shape)} "
                          f"on {t.device}")
     width = shape[-1] * shape[-2]
     if t.is_contiguous():
@@ -440,75 +444,57 @@ def _expect_rows(t, name, shape, dtype, device):
     return t.data_ptr(), width if row is None else row
 
 
-def _cache(k_pool, v_pool, page_table, layered: bool) -> bpd_cache:
-    import torch
-    dims = 5 if layered else 4
-    if k_pool.dim() != dims or k_pool.shape[-3] != 64:
-        raise ValueError(f"pools: expected [{'layers, ' if layered else ''}pages, 64, kv_heads, head_dim], got {tuple(k_pool.shape)}")
-    if k_pool.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError(f"pools: expected float32 or bfloat16, got {k_pool.dtype}")
-    if page_table.dim() != 2:
-        raise ValueError(f"page_table: expected [batch, pages_per_row], got {tuple(page_table.shape)}")
-    device, shape = k_pool.device, k_pool.shape
-    if device.type != "cuda":
-        raise ValueError(f"pools: expected CUDA tensors, got {device}")
-    c = bpd_cache()
-    c.k_pool = _expect(k_pool, "k_pool", shape, k_pool.dtype, device)
-    c.v_pool = None if v_pool is None else _expect(v_pool, "v_pool", shape, k_pool.dtype, device)
-    c.page_table = _expect(page_table, "page_table", page_table.shape, torch.int32, device)
-    c.layers = shape[0] if layered else 1
-    c.n_pages, c.kv_heads, c.head_dim = shape[-4], shape[-2], shape[-1]
-    c.batch, c.pages_per_row = page_table.shape
-    c.dtype = 0 if k_pool.dtype == torch.float32 else 1
-    return c
+def _cache(k_pool, v_pool, page_table, layered: bool):
+    """The structure of the calls, and the pool's shape, type and device index."""
+    shape, dtype, device = k_pool.shape, k_pool.dtype, k_pool.get_device()
+    if len(shape) != (5 if layered else 4) or shape[-3] != 64:
+        raise ValueError(f"pools: expected [{'layers, ' if layered else ''}pages, 64, kv_heads, head_dim], got {tuple(shape)}")
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+        raise ValueError(f"pools: expected float32 or bfloat16, got {dtype}")
+    rows = page_table.shape
+    if len(rows) != 2:
+        raise ValueError(f"page_table: expected [batch, pages_per_row], got {tuple(rows)}")
+    if not k_pool.is_cuda:
+        raise ValueError(f"pools: expected CUDA tensors, got {k_pool.device}")
+    return bpd_cache(_expect(k_pool, "k_pool", shape, dtype, device), None if v_pool is None else _expect(v_pool, "v_pool", shape, dtype, device),
+                     _expect(page_table, "page_table", rows, torch.int32, device), shape[0] if layered else 1, shape[-4], rows[1], rows[0],
+                     shape[-2], shape[-1], 0 if dtype is torch.float32 else 1), shape, dtype, device
 
 
-class _On:
-    """The device that a call's tensors are on, made current for the call, and its current stream."""
-
-    def __init__(self, device):
-        self.index = device.index
-
-    def __enter__(self):
-        import torch
-        self.before = torch.cuda.current_device()
-        if self.before != self.index:
-            torch.cuda.set_device(self.index)
-        return torch._C._cuda_getCurrentRawStream(self.index)
-
-    def __exit__(self, *exc):
-        if self.before != self.index:
-            import torch
-            torch.cuda.set_device(self.before)
+def _enqueue(device: int, fn, *args):
+    """The call on the current stream of this device, with the device current."""
+    if torch._C._cuda_getDevice() == device:
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(device))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(device))
+    if rc != BPD_OK:
+        _check(rc)
 
 
-def _drafted(c, q, k_new, v_new, lens, parents, nodes):
-    """Checks of what both attentions take; (addresses and strides in the order of the calls)."""
-    import torch
-    device, dtype = q.device, q.dtype
-    if q.dim() != 4:
-        raise ValueError(f"q: expected [batch, nodes, heads, head_dim], got {tuple(q.shape)}")
-    t, h = q.shape[1], q.shape[2]
-    qp, qs = _expect_rows(q, "q", (c.batch, t, h, c.head_dim), dtype, device)
-    kp, ks = _expect_rows(k_new, "k_new", (c.batch, t, c.kv_heads, c.head_dim), dtype, device)
-    vp, vs = _expect_rows(v_new, "v_new", (c.batch, t, c.kv_heads, c.head_dim), dtype, device)
-    if ks != vs:
-        raise ValueError(f"k_new and v_new: rows must be the same stride apart, got {ks} and {vs}")
-    i32 = torch.int32
-    return (qp, kp, vp, t, h, qs, ks, _expect(lens, "lens", (c.batch,), i32, device), _expect(parents, "parents", (c.batch, t), i32, device),
-            None if nodes is None else _expect(nodes, "nodes", (c.batch,), i32, device))
-
-
-def _same_kind(q, k_pool):
-    if q.dtype != k_pool.dtype or q.device != k_pool.device:
-        raise ValueError(f"q is {q.dtype} on {q.device}, the cache {k_pool.dtype} on {k_pool.device}")
-
-
-def _scratch_bytes(n: int) -> int:
-    """The size a scratch_bytes call answered; 0 is its refusal."""
+def _scratch(like, n: int):
+    """n bytes on a tensor's device; 0 is the refusal of the scratch_bytes call that answered it."""
     if n == 0:
         raise BpdError(-2, lib.bpd_last_error().decode(errors="replace"))
-    return n
+    return like.new_empty(n, dtype=torch.uint8)
+
+
+def _drafted(cache, q, k_new, v_new, lens, parents, nodes):
+    """Checks of what both attentions take: addresses, sizes and strides in the order of the calls."""
+    c, pool, dtype, device = cache
+    if q.dim() != 4:
+        raise ValueError(f"q: expected [batch, nodes, heads, head_dim], got {tuple(q.shape)}")
+    _, t, h, _ = q.shape
+    b, hk, d = lens.shape[0] if lens.dim() == 1 else -1, pool[-2], pool[-1]
+    if b != c.batch:
+        raise ValueError(f"lens: expected [{c.batch}] as the page table has rows, got {tuple(lens.shape)}")
+    qp, qs = _expect_rows(q, "q", (b, t, h, d), dtype, device)
+    kp, ks = _expect_rows(k_new, "k_new", (b, t, hk, d), dtype, device)
+    vp, vs = _expect_rows(v_new, "v_new", (b, t, hk, d), dtype, device)
+    if ks != vs:
+        raise ValueError(f"k_new and v_new: rows must be the same stride apart, got {ks} and {vs}")
+    return (qp, kp, vp, t, h, qs, ks, _expect(lens, "lens", (b,), torch.int32, device), _expect(parents, "parents", (b, t), torch.int32, device),
+            None if nodes is None else _expect(nodes, "nodes", (b,), torch.int32, device))
 
 
 def bpd_op_tree_attention(q, k_new, v_new, k_pool, v_pool, page_table, lens, parents, nodes=None, scale: Optional[float] = None,
@@ -516,17 +502,14 @@ def bpd_op_tree_attention(q, k_new, v_new, k_pool, v_pool, page_table, lens, par
     """Attention of drafted nodes over one layer's cache and their own tree: see include/bpd.h.  q [batch, nodes, heads, head_dim],
     k_new, v_new [batch, nodes, kv_heads, head_dim] (slices of a fused projection will do), lens, nodes int32 [batch], parents
     int32 [batch, nodes].  scale: head_dim ** -0.5 if not given.  Returns out (and lse)."""
-    import torch
-    c = _cache(k_pool, v_pool, page_table, False)
-    _same_kind(q, k_pool)
-    args = _drafted(c, q, k_new, v_new, lens, parents, nodes)
-    with _On(q.device) as stream:
-        n = _scratch_bytes(lib.bpd_op_tree_attention_scratch_bytes(C.byref(c), args[3], args[4]))
-        scratch = torch.empty(n, dtype=torch.uint8, device=q.device)
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if want_lse else None
-        _check(lib.bpd_op_tree_attention(C.byref(c), *args, c.head_dim ** -0.5 if scale is None else scale, scratch.data_ptr(), n,
-                                         out.data_ptr(), None if lse is None else lse.data_ptr(), stream))
+    cache = _cache(k_pool, v_pool, page_table, False)
+    args = _drafted(cache, q, k_new, v_new, lens, parents, nodes)
+    c = C.byref(cache[0])
+    n = lib.bpd_op_tree_attention_scratch_bytes(c, args[3], args[4])
+    scratch, out = _scratch(q, n), q.new_empty(*q.shape)
+    lse = q.new_empty(*q.shape[:3], dtype=torch.float32) if want_lse else None
+    _enqueue(cache[3], lib.bpd_op_tree_attention, c, *args, q.shape[3] ** -0.5 if scale is None else scale, scratch.data_ptr(), n, out.data_ptr(),
+             lse.data_ptr() if want_lse else None)
     return (out, lse) if want_lse else out
 
 
@@ -534,98 +517,84 @@ def bpd_op_page_attention(q, k_new, v_new, k_pool, v_pool, page_table, means, le
                           scale: Optional[float] = None, want_lse: bool = False, want_pages: bool = False):
     """bpd_op_tree_attention over the ``select`` best full pages for each node and key head, the open page and the node's line.
     means: float32 [batch, pages_per_row, kv_heads, head_dim].  Returns out, then lse and pages where wanted."""
-    import torch
-    c = _cache(k_pool, v_pool, page_table, False)
-    _same_kind(q, k_pool)
-    args = _drafted(c, q, k_new, v_new, lens, parents, nodes)
-    mp = _expect(means, "means", (c.batch, c.pages_per_row, c.kv_heads, c.head_dim), torch.float32, q.device)
+    cache = _cache(k_pool, v_pool, page_table, False)
+    args = _drafted(cache, q, k_new, v_new, lens, parents, nodes)
+    (b, per_row), (hk, d), t = page_table.shape, cache[1][-2:], args[3]
+    mp = _expect(means, "means", (b, per_row, hk, d), torch.float32, cache[3])
     if select < 1:
         raise ValueError(f"select must be at least 1, got {select}")
-    n_sel = min(select, c.pages_per_row)
-    with _On(q.device) as stream:
-        n = _scratch_bytes(lib.bpd_op_page_attention_scratch_bytes(C.byref(c), args[3], args[4], n_sel))
-        scratch = torch.empty(n, dtype=torch.uint8, device=q.device)
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if want_lse else None
-        pages = torch.empty((c.batch, args[3], c.kv_heads, n_sel), dtype=torch.int32, device=q.device) if want_pages else None
-        _check(lib.bpd_op_page_attention(C.byref(c), mp, *args, n_sel, c.head_dim ** -0.5 if scale is None else scale,
-                                         scratch.data_ptr(), n, out.data_ptr(), None if lse is None else lse.data_ptr(),
-                                         None if pages is None else pages.data_ptr(), stream))
-        if want_pages and n_sel < select:
-            pages = torch.nn.functional.pad(pages, (0, select - n_sel), value=-1)
-    got = (out,) + ((lse,) if want_lse else ()) + ((pages,) if want_pages else ())
-    return got if len(got) > 1 else out
+    n_sel = min(select, per_row)
+    c = C.byref(cache[0])
+    n = lib.bpd_op_page_attention_scratch_bytes(c, t, args[4], n_sel)
+    scratch, out = _scratch(q, n), q.new_empty(*q.shape)
+    lse = q.new_empty(*q.shape[:3], dtype=torch.float32) if want_lse else None
+    pages = lens.new_empty(b, t, hk, n_sel) if want_pages else None
+    _enqueue(cache[3], lib.bpd_op_page_attention, c, mp, *args, n_sel, d ** -0.5 if scale is None else scale, scratch.data_ptr(), n, out.data_ptr(),
+             lse.data_ptr() if want_lse else None, pages.data_ptr() if want_pages else None)
+    if want_pages and n_sel < select:
+        pages = torch.nn.functional.pad(pages, (0, select - n_sel), value=-1)
+    if not want_lse and not want_pages:
+        return out
+    return (out,) + ((lse,) if want_lse else ()) + ((pages,) if want_pages else ())
 
 
 def bpd_op_tree_commit(k_new, v_new, k_pool, v_pool, page_table, lens, parents, tokens, top1, last_top1, nodes=None, eos_id: int = -1):
     """Walks every row's tree along the base model's predictions and writes the accepted nodes' keys and values to the caches of
     all layers.  k_new, v_new [layers, batch, nodes, kv_heads, head_dim]; pools with layers.  Returns the new lengths, accepted
     counts, paths [batch, nodes] and the predictions after the paths."""
-    import torch
-    c = _cache(k_pool, v_pool, page_table, True)
+    c, pool, dtype, device = _cache(k_pool, v_pool, page_table, True)
     if parents.dim() != 2:
         raise ValueError(f"parents: expected [batch, nodes], got {tuple(parents.shape)}")
-    device, i32, t = k_pool.device, torch.int32, parents.shape[1]
-    shape = (c.layers, c.batch, t, c.kv_heads, c.head_dim)
-    kp, ks = _expect_rows(k_new, "k_new", shape, k_pool.dtype, device)
-    vp, vs = _expect_rows(v_new, "v_new", shape, k_pool.dtype, device)
+    b, t, i32 = page_table.shape[0], parents.shape[1], torch.int32
+    shape = (pool[0], b, t, pool[3], pool[4])
+    kp, ks = _expect_rows(k_new, "k_new", shape, dtype, device)
+    vp, vs = _expect_rows(v_new, "v_new", shape, dtype, device)
     if ks != vs:
         raise ValueError(f"k_new and v_new: rows must be the same stride apart, got {ks} and {vs}")
-    ints = [_expect(x, name, (c.batch, t), i32, device) for x, name in ((parents, "parents"), (tokens, "tokens"), (top1, "top1"))]
-    lp, tp = _expect(lens, "lens", (c.batch,), i32, device), _expect(last_top1, "last_top1", (c.batch,), i32, device)
-    np_ = None if nodes is None else _expect(nodes, "nodes", (c.batch,), i32, device)
-    with _On(device) as stream:
-        out = torch.empty((3, c.batch), dtype=i32, device=device)
-        path = torch.empty((c.batch, t), dtype=i32, device=device)
-        new_lens, accepted, following = out.unbind(0)
-        _check(lib.bpd_op_tree_commit(C.byref(c), kp, vp, t, ks, lp, *ints, tp, np_, eos_id, new_lens.data_ptr(), accepted.data_ptr(),
-                                      path.data_ptr(), following.data_ptr(), stream))
+    args = (_expect(lens, "lens", (b,), i32, device), _expect(parents, "parents", (b, t), i32, device), _expect(tokens, "tokens", (b, t), i32, device),
+            _expect(top1, "top1", (b, t), i32, device), _expect(last_top1, "last_top1", (b,), i32, device),
+            None if nodes is None else _expect(nodes, "nodes", (b,), i32, device))
+    new_lens, accepted, following, path = lens.new_empty(b), lens.new_empty(b), lens.new_empty(b), lens.new_empty(b, t)
+    _enqueue(device, lib.bpd_op_tree_commit, C.byref(c), kp, vp, t, ks, *args, eos_id, new_lens.data_ptr(), accepted.data_ptr(), path.data_ptr(),
+             following.data_ptr())
     return new_lens, accepted, path, following
 
 
 def bpd_op_cache_weights(q, lse, path, accepted, k_pool, page_table, lens, seen, weights, positions, scale: Optional[float] = None):
     """Adds the attention weights of the accepted nodes to ``weights`` and numbers their own entries in ``positions`` (both
     [batch, kv_heads, capacity], in place).  One layer's pool; ``lens`` are the lengths before the commit."""
-    import torch
-    c = _cache(k_pool, None, page_table, False)
-    _same_kind(q, k_pool)
+    c, pool, dtype, device = _cache(k_pool, None, page_table, False)
     if q.dim() != 4:
         raise ValueError(f"q: expected [batch, nodes, heads, head_dim], got {tuple(q.shape)}")
-    device, i32, (t, h) = q.device, torch.int32, q.shape[1:3]
-    qp, qs = _expect_rows(q, "q", (c.batch, t, h, c.head_dim), q.dtype, device)
-    state = (c.batch, c.kv_heads, c.pages_per_row * 64)
-    args = (_expect(lse, "lse", (c.batch, t, h), torch.float32, device), _expect(path, "path", (c.batch, t), i32, device),
-            _expect(accepted, "accepted", (c.batch,), i32, device), _expect(lens, "lens", (c.batch,), i32, device),
-            _expect(seen, "seen", (c.batch,), i32, device), c.head_dim ** -0.5 if scale is None else scale,
-            _expect(weights, "weights", state, torch.float32, device), _expect(positions, "positions", state, i32, device))
-    with _On(device) as stream:
-        _check(lib.bpd_op_cache_weights(C.byref(c), qp, t, h, qs, *args, stream))
+    (b, per_row), (_, t, h, _), (hk, d), i32 = page_table.shape, q.shape, pool[-2:], torch.int32
+    qp, qs = _expect_rows(q, "q", (b, t, h, d), dtype, device)
+    state = (b, hk, per_row * 64)
+    _enqueue(device, lib.bpd_op_cache_weights, C.byref(c), qp, t, h, qs, _expect(lse, "lse", (b, t, h), torch.float32, device),
+             _expect(path, "path", (b, t), i32, device), _expect(accepted, "accepted", (b,), i32, device), _expect(lens, "lens", (b,), i32, device),
+             _expect(seen, "seen", (b,), i32, device), d ** -0.5 if scale is None else scale,
+             _expect(weights, "weights", state, torch.float32, device), _expect(positions, "positions", state, i32, device))
 
 
 def bpd_op_cache_evict(weights, positions, k_pool, v_pool, page_table, lens, seen, budget: int, recent: int = 0):
     """Leaves at most ``budget`` entries in every list (layer, row, key head): the last ``recent`` tokens, then the heaviest.
     weights, positions [layers, batch, kv_heads, capacity] and the pools (with layers) change in place.  Returns the new lengths."""
-    import torch
-    c = _cache(k_pool, v_pool, page_table, True)
-    device, i32 = k_pool.device, torch.int32
-    state = (c.layers, c.batch, c.kv_heads, c.pages_per_row * 64)
+    c, pool, _, device = _cache(k_pool, v_pool, page_table, True)
+    (b, per_row), i32 = page_table.shape, torch.int32
+    state = (pool[0], b, pool[3], per_row * 64)
     wp, pp = _expect(weights, "weights", state, torch.float32, device), _expect(positions, "positions", state, i32, device)
-    lp, sp = _expect(lens, "lens", (c.batch,), i32, device), _expect(seen, "seen", (c.batch,), i32, device)
-    with _On(device) as stream:
-        n = _scratch_bytes(lib.bpd_op_cache_evict_scratch_bytes(C.byref(c), budget))
-        scratch = torch.empty(n, dtype=torch.uint8, device=device)
-        out = torch.empty(c.batch, dtype=i32, device=device)
-        _check(lib.bpd_op_cache_evict(C.byref(c), lp, sp, budget, recent, wp, pp, scratch.data_ptr(), n, out.data_ptr(), stream))
+    lp, sp = _expect(lens, "lens", (b,), i32, device), _expect(seen, "seen", (b,), i32, device)
+    ref = C.byref(c)
+    n = lib.bpd_op_cache_evict_scratch_bytes(ref, budget)
+    scratch, out = _scratch(weights, n), lens.new_empty(b)
+    _enqueue(device, lib.bpd_op_cache_evict, ref, lp, sp, budget, recent, wp, pp, scratch.data_ptr(), n, out.data_ptr())
     return out
 
 
 def bpd_op_page_means(k_pool, page_table, lens_from, lens, means):
     """Means of the keys of the pages that became full between two lengths, into ``means`` float32 [layers, batch, pages_per_row,
     kv_heads, head_dim].  Pool with layers."""
-    import torch
-    c = _cache(k_pool, None, page_table, True)
-    device, i32 = k_pool.device, torch.int32
-    mp = _expect(means, "means", (c.layers, c.batch, c.pages_per_row, c.kv_heads, c.head_dim), torch.float32, device)
-    fp, lp = _expect(lens_from, "lens_from", (c.batch,), i32, device), _expect(lens, "lens", (c.batch,), i32, device)
-    with _On(device) as stream:
-        _check(lib.bpd_op_page_means(C.byref(c), fp, lp, mp, stream))
+    c, pool, _, device = _cache(k_pool, None, page_table, True)
+    b, per_row = page_table.shape
+    mp = _expect(means, "means", (pool[0], b, per_row, pool[3], pool[4]), torch.float32, device)
+    _enqueue(device, lib.bpd_op_page_means, C.byref(c), _expect(lens_from, "lens_from", (b,), torch.int32, device),
+             _expect(lens, "lens", (b,), torch.int32, device), mp)

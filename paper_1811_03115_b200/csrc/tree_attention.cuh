@@ -12,8 +12,8 @@
 // tile leaves a partial result (maximum, sum, unnormalised output) in the scratch; combine_kernel joins those.
 //
 // Precision: bf16 caches: scores are exact products summed in fp32; softmax weights go into the second product as two bf16
-// planes (w = h + l, 16 bits of mantissa), so the output's error is its own rounding to bf16 (with one plane it was 1.4
-// times that).  fp32 caches: every operand is three bf16 planes (24 bits), the six largest of the nine products are taken
+// planes (w = h + l, 16 bits of mantissa), so the output's error is its own rounding to bf16 (one plane's rounding would add
+// as much again).  fp32 caches: every operand is three bf16 planes (24 bits), the six largest of the nine products are taken
 // (the rest is below 2^-24), and outputs are summed per chunk in the tensor core but across chunks by fp32 FMAs (the tensor
 // core's own additions truncate).
 #pragma once
@@ -42,6 +42,9 @@ struct AttnArgs {
   void* out;                                   // [B][T][H][D]
   float* lse;                                  // [B][T][H] or null
   float* part;                                 // [ctas][2][R * (D + 2)]
+  int split;                                   // 1: equal runs of chunks, joined by combine_kernel; 0: a tile per CTA
+  int part_rows;                               // rows of a partial result
+  int ctas;                                    // CTAs of the launch
   int2* info;                                  // per tile: 2 * first CTA that has units of it + the slot of its partial result; last CTA
 };
 
@@ -77,7 +80,6 @@ struct Shape {
   static constexpr int RING = STAGES * Rows<CT, D>::STAGE;
   static constexpr int SMEM = Q_BYTES + (RING > MERGE ? RING : MERGE);
   static constexpr int CTAS_PER_SM = F32 ? (D >= 128 ? 1 : 2) : (D >= 128 ? 2 : 3);
-  static constexpr int PART = R * (D + 2);                  // floats of a partial result
 };
 
 // Bits of the ancestors-or-self of node t among nodes 64 * word .. 64 * word + 63.
@@ -89,6 +91,9 @@ __device__ __forceinline__ unsigned long long line_bits(const int* parents, int 
   }
   return bits;
 }
+
+// Floats of a partial result: outputs [rows][D], maxima, sums; whole 16 bytes, as the outputs go there four at a time.
+__host__ __device__ __forceinline__ long long part_floats(int rows, int D) { return ((long long)rows * (D + 2) + 3) / 4 * 4; }
 
 struct Seq { int len, nodes; SeqWork w; };
 
@@ -137,14 +142,132 @@ __device__ __forceinline__ void split2_pair(float x, float y, uint32_t& hi, uint
   lo = *reinterpret_cast<const uint32_t*>(&l);
 }
 
-// Sum over the block; every thread gets it.  `box`: one slot per warp.
-__device__ __forceinline__ long long block_sum(long long v, long long* box) {
+// A CTA's way through its work, tile by tile.  Every warp keeps one of its own: what it needs of a batch's lengths a warp
+// finds out alone, without a barrier.
+template <bool PAGED>
+struct Walk {
+  const AttnArgs& a;
+  const int tile_rows;
+  long long units, ctas, u_begin, u, u_end, seq_first;
+  int b;
+  Seq sq;
+  Tile tl;
+  int c_begin, c_end;        // chunks of the tile to work on
+  int slot, last_cta;        // of the partial result; the CTA that has the tile's last chunk
+
+  __device__ __forceinline__ Walk(const AttnArgs& args, int rows) : a(args), tile_rows(rows) {}
+  __device__ __forceinline__ long long units_of(int i) const {
+    const SeqWork w = seq_of<PAGED>(a, i, tile_rows).w;
+    return (long long)w.tiles * w.chunks;
+  }
+  // False if there is nothing for this CTA.
+  __device__ __forceinline__ bool begin() {
+    if (!a.split) {
+      const int rt = PAGED ? ceil_div(a.G, tile_rows) : ceil_div(a.T * a.G, tile_rows);
+      int id = blockIdx.x;
+      tl.id = id;
+      tl.r0 = id % rt * tile_rows;
+      id /= rt;
+      tl.h = id % a.Hkv;
+      id /= a.Hkv;
+      tl.t = PAGED ? id % a.T : 0;
+      b = PAGED ? id / a.T : id;
+      sq = seq_of<PAGED>(a, b, tile_rows);
+      c_begin = 0;
+      c_end = sq.w.chunks;
+      return PAGED ? tl.t < sq.nodes : tl.r0 < sq.nodes * a.G;
+    }
+    const int lane = threadIdx.x & 31;
+    long long sum = 0;
+    for (int i = lane; i < a.B; i += 32) sum += units_of(i);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) box[threadIdx.x >> 5] = v;
-  __syncthreads();
-  return box[0] + box[1] + box[2] + box[3];
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    units = sum;
+    ctas = min(units, (long long)gridDim.x);                // no CTA that shares a tile may be without a unit
+    if (blockIdx.x >= ctas) return false;
+    u = u_begin = first_unit(blockIdx.x, units, ctas);
+    u_end = first_unit(blockIdx.x + 1, units, ctas);
+    long long before = 0;
+    for (int b0 = 0;; b0 += 32) {
+      const long long n = b0 + lane < a.B ? units_of(b0 + lane) : 0;
+      long long upto = n;                                   // inclusive scan
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) { const long long x = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += x; }
+      const unsigned hit = __ballot_sync(0xffffffffu, before + upto > u_begin);
+      if (hit) {
+        const int at = __ffs(hit) - 1;
+        b = b0 + at;
+        seq_first = before + __shfl_sync(0xffffffffu, upto - n, at);
+        break;
+      }
+      before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    sq = seq_of<PAGED>(a, b, tile_rows);
+    find();
+    return true;
+  }
+  // The next tile; false if the CTA's run is done.
+  __device__ __forceinline__ bool next() {
+    if (!a.split) return false;
+    u += c_end - c_begin;
+    if (u >= u_end) return false;
+    while (u >= seq_first + (long long)sq.w.tiles * sq.w.chunks) {
+      seq_first += (long long)sq.w.tiles * sq.w.chunks;
+      sq = seq_of<PAGED>(a, ++b, tile_rows);
+    }
+    find();
+    return true;
+  }
+  __device__ __forceinline__ void find() {
+    const int local = (int)((u - seq_first) / sq.w.chunks);
+    const long long tile_first = seq_first + (long long)local * sq.w.chunks;
+    c_begin = (int)(u - tile_first);
+    c_end = (int)min((long long)sq.w.chunks, u_end - tile_first);
+    tl = tile_of<PAGED>(a, b, sq.nodes, local, tile_rows);
+    slot = u == u_begin ? 0 : 1;                            // a CTA leaves at most two partial results: of its first tile, of its last
+    last_cta = c_begin == 0 && c_end < sq.w.chunks ? cta_of_unit(tile_first + sq.w.chunks - 1, units, ctas) : (int)blockIdx.x;
+  }
+  __device__ __forceinline__ int rows() const { return PAGED ? min(tile_rows, a.G - tl.r0) : min(tile_rows, sq.nodes * a.G - tl.r0); }
+  // node and head of row r of the tile, and its row of the output
+  __device__ __forceinline__ int node_of(int r) const { return PAGED ? tl.t : (tl.r0 + r) / a.G; }
+  __device__ __forceinline__ int head_of(int r) const { return tl.h * a.G + (PAGED ? tl.r0 + r : (tl.r0 + r) % a.G); }
+  __device__ __forceinline__ long long out_row(int r) const { return ((long long)b * a.T + node_of(r)) * a.H + head_of(r); }
+  __device__ __forceinline__ int tree_chunks() const { return ceil_div(sq.nodes, kChunk); }
+  __device__ __forceinline__ int cache_chunks() const { return sq.w.chunks - ceil_div(sq.nodes, kChunk); }
+  __device__ __forceinline__ bool whole() const { return c_begin == 0 && c_end == sq.w.chunks; }
+  // Page of cache chunk c (-1: none, or a chunk of the tree), and the number of keys in a chunk.
+  __device__ __forceinline__ int page_of(int c) const {
+    const int cached = cache_chunks(), full = sq.len / kPagePos;
+    if (c >= cached) return -1;
+    int logical = c;
+    if (PAGED && c < cached - (sq.len % kPagePos ? 1 : 0)) {
+      logical = a.pages[((long long)(b * a.T + tl.t) * a.Hkv + tl.h) * a.select + c];
+      if (logical < 0 || logical >= full) return -1;
+    } else if (PAGED) {
+      logical = full;
+    }
+    const int page = a.table[(long long)b * a.ppr + logical];
+    return pool_row(page, a.n_pages, 0) < 0 ? -1 : page;
+  }
+  __device__ __forceinline__ int keys_of(int c, int page) const {
+    const int cached = cache_chunks();
+    if (c >= cached) return min(kChunk, sq.nodes - (c - cached) * kChunk);
+    if (page < 0) return 0;
+    const bool open = sq.len % kPagePos && c == cached - 1;
+    return open ? sq.len % kPagePos : kChunk;
+  }
+};
+
+// Rows behind a sequence's last node: zeros, and a log-sum of nothing.
+template <typename CT>
+__device__ __forceinline__ void clear_dead_rows(const AttnArgs& a, int D) {
+  if (!a.nodes) return;
+  for (int i = blockIdx.x; i < a.B * a.T; i += gridDim.x) {
+    if (i % a.T < clamp_int(a.nodes[i / a.T], 0, a.T)) continue;
+    CT* o = reinterpret_cast<CT*>(a.out) + (long long)i * a.H * D;
+    for (int c = threadIdx.x * 4; c < a.H * D; c += blockDim.x * 4) store4<CT>(o + c, make_float4(0.f, 0.f, 0.f, 0.f));
+    if (a.lse) for (int c = threadIdx.x; c < a.H; c += blockDim.x) a.lse[(long long)i * a.H + c] = -INFINITY;
+  }
 }
 
 template <typename CT, int D, int WR, bool PAGED>
@@ -155,9 +278,7 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
   constexpr bool F32 = S::F32;
   constexpr int R = S::R, WK = S::WK, KW = S::KW, KT = D / 16, NT = KW / 8, DT = D / 8;
   extern __shared__ __align__(128) uint8_t ta_smem[];
-  __shared__ long long s_box[4];
-  __shared__ long long s_at;            // first unit of the sequence the CTA begins in
-  __shared__ int s_b, s_keys[S::STAGES], s_parents[kMaxNodes];
+  __shared__ int s_keys[S::STAGES], s_parents[kMaxNodes];
   __shared__ unsigned long long s_line[R][kMaxNodes / 64];
   __shared__ float s_m[WK][R], s_l[WK][R];
   bf16* qs = reinterpret_cast<bf16*>(ta_smem);
@@ -166,83 +287,20 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
   const int wr = warp % WR, wk = warp / WR;
 
-  // rows behind a sequence's last node: zeros, and a log-sum of nothing
-  if (a.nodes) {
-    for (int i = blockIdx.x; i < a.B * a.T; i += gridDim.x) {
-      if (i % a.T < clamp_int(a.nodes[i / a.T], 0, a.T)) continue;
-      CT* o = reinterpret_cast<CT*>(a.out) + (long long)i * a.H * D;
-      for (int c = tid * 4; c < a.H * D; c += kThreads * 4) store4<CT>(o + c, make_float4(0.f, 0.f, 0.f, 0.f));
-      if (a.lse) for (int c = tid; c < a.H; c += kThreads) a.lse[(long long)i * a.H + c] = -INFINITY;
-    }
-  }
-
-  // this CTA's run of units, and the sequence it begins in
-  long long mine = 0;
-  for (int b = tid; b < a.B; b += kThreads) { const SeqWork w = seq_of<PAGED>(a, b, R).w; mine += (long long)w.tiles * w.chunks; }
-  const long long units = block_sum(mine, s_box);
-  const long long ctas = min(units, (long long)gridDim.x);  // no CTA that shares a tile may be without a unit
-  if (blockIdx.x >= ctas) return;
-  const long long u_begin = first_unit(blockIdx.x, units, ctas), u_end = first_unit(blockIdx.x + 1, units, ctas);
-  long long before = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kThreads) {
-    const int b = b0 + tid;
-    long long n = 0;
-    if (b < a.B) { const SeqWork w = seq_of<PAGED>(a, b, R).w; n = (long long)w.tiles * w.chunks; }
-    long long upto = n;                                     // inclusive scan over the block
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const long long x = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += x; }
-    __syncthreads();
-    if (lane == 31) s_box[warp] = upto;
-    __syncthreads();
-    long long base = before;
-    for (int w = 0; w < warp; ++w) base += s_box[w];
-    if (n > 0 && base + upto - n <= u_begin && u_begin < base + upto) { s_b = b; s_at = base + upto - n; }
-    before += s_box[0] + s_box[1] + s_box[2] + s_box[3];
-    __syncthreads();
-    if (before > u_begin) break;
-  }
-  int b = s_b;
-  long long seq_first = s_at, u = u_begin;
-  Seq sq = seq_of<PAGED>(a, b, R);
+  clear_dead_rows<CT>(a, D);
+  Walk<PAGED> w(a, R);
+  if (!w.begin()) return;
   int lines_of = -1;                                        // sequence whose parents are in shared memory
 
-  while (u < u_end) {
-    while (u >= seq_first + (long long)sq.w.tiles * sq.w.chunks) {
-      seq_first += (long long)sq.w.tiles * sq.w.chunks;
-      sq = seq_of<PAGED>(a, ++b, R);
-    }
-    const int local = (int)((u - seq_first) / sq.w.chunks);
-    const long long tile_first = seq_first + (long long)local * sq.w.chunks;
-    const int c_begin = (int)(u - tile_first), c_end = (int)min((long long)sq.w.chunks, u_end - tile_first);
-    const Tile tl = tile_of<PAGED>(a, b, sq.nodes, local, R);
-    const int rows = PAGED ? min(R, a.G - tl.r0) : min(R, sq.nodes * a.G - tl.r0);
-    const int tree_chunks = ceil_div(sq.nodes, kChunk), cache_chunks = sq.w.chunks - tree_chunks;
-    const int full = sq.len / kPagePos;
-    const int* table = a.table + (long long)b * a.ppr;
-    const int* sel = PAGED ? a.pages + ((long long)(b * a.T + tl.t) * a.Hkv + tl.h) * a.select : nullptr;
-    // node and head of row r of the tile
-    auto node_of = [&](int r) { return PAGED ? tl.t : (tl.r0 + r) / a.G; };
-    auto head_of = [&](int r) { return tl.h * a.G + (PAGED ? tl.r0 + r : (tl.r0 + r) % a.G); };
-
-    // page and keys of cache chunk c (page -1: none)
-    auto page_of = [&](int c) -> int {
-      if (c >= cache_chunks) return -1;
-      int logical = c;
-      if (PAGED && c < cache_chunks - (sq.len % kPagePos ? 1 : 0)) {
-        logical = sel[c];
-        if (logical < 0 || logical >= full) return -1;
-      } else if (PAGED) {
-        logical = full;
-      }
-      const int page = table[logical];
-      return pool_row(page, a.n_pages, 0) < 0 ? -1 : page;
-    };
-    auto keys_of = [&](int c, int page) -> int {
-      if (c >= cache_chunks) return min(kChunk, sq.nodes - (c - cache_chunks) * kChunk);
-      if (page < 0) return 0;
-      const bool open = PAGED ? c == cache_chunks - 1 && sq.len % kPagePos : c == full;
-      return open ? sq.len % kPagePos : kChunk;
-    };
+  do {
+    const int rows = w.rows(), b = w.b, cache_chunks = w.cache_chunks(), c_begin = w.c_begin, c_end = w.c_end;
+    auto page_of = [&](int c) { return w.page_of(c); };
+    auto keys_of = [&](int c, int page) { return w.keys_of(c, page); };
+    auto node_of = [&](int r) { return w.node_of(r); };
+    auto head_of = [&](int r) { return w.head_of(r); };
+    const Tile& tl = w.tl;
+    const Seq& sq = w.sq;
+    const int tree_chunks = w.tree_chunks();
     auto load = [&](int c, int page, int stage) {
       const CT *k, *v;
       long long step;
@@ -534,9 +592,8 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
       *reinterpret_cast<float2*>(at + 8 * S::MP) = make_float2(o[n][2], o[n][3]);
     }
     __syncthreads();
-    const bool whole = c_begin == 0 && c_end == sq.w.chunks;
-    const int slot = u == u_begin ? 0 : 1;                  // a CTA leaves at most two partial results: of its first tile, of its last
-    float* part = a.part + ((long long)blockIdx.x * 2 + slot) * S::PART;
+    const bool whole = w.whole();
+    float* part = a.part + ((long long)blockIdx.x * 2 + (a.split ? w.slot : 0)) * part_floats(a.part_rows, D);
     for (int i = tid; i < rows * (D / 4); i += kThreads) {
       const int r = i / (D / 4), c4 = i % (D / 4) * 4;
       float m = s_m[0][r];
@@ -554,26 +611,24 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
       }
       if (whole) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        const long long at = ((long long)b * a.T + node_of(r)) * a.H + head_of(r);
+        const long long at = w.out_row(r);
         store4<CT>(reinterpret_cast<CT*>(a.out) + at * D + c4, make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv));
         if (a.lse && c4 == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945f;
       } else {
         *reinterpret_cast<float4*>(part + r * D + c4) = x;
-        if (c4 == 0) { part[R * D + r] = m; part[R * D + R + r] = l; }
+        if (c4 == 0) { part[a.part_rows * D + r] = m; part[a.part_rows * (D + 1) + r] = l; }
       }
     }
-    if (c_begin == 0 && tid == 0)
-      a.info[tl.id] = make_int2(blockIdx.x * 2 + slot, cta_of_unit(tile_first + sq.w.chunks - 1, units, ctas));
+    if (!a.split) return;
+    if (c_begin == 0 && tid == 0) a.info[tl.id] = make_int2(blockIdx.x * 2 + w.slot, w.last_cta);
     __syncthreads();                                        // the ring, the lines and the sums are free again
-    u = tile_first + c_end;
-  }
+  } while (w.next());
 }
 
 // Joins the partial results of the tiles that more than one CTA worked on.  grid: (tiles that could be, R / 4), a warp per row.
-template <typename CT, int D, int WR, bool PAGED>
-__global__ void __launch_bounds__(kThreads) combine_kernel(const __grid_constant__ AttnArgs a) {
-  using S = Shape<CT, D, WR>;
-  constexpr int R = S::R;
+template <typename CT, int D, bool PAGED>
+__global__ void __launch_bounds__(kThreads) combine_kernel(const __grid_constant__ AttnArgs a, int tile_rows) {
+  const int R = tile_rows, PR = a.part_rows;
   pdl_wait();                                               // (every CTA: the launch after this one waits for this one alone)
   const int id = blockIdx.x, r = blockIdx.y * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   int b, h, t, r0;
@@ -589,24 +644,44 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(const __grid_constant
   if (r0 + r >= rows) return;
   const int node = PAGED ? t : (r0 + r) / a.G, head = h * a.G + (PAGED ? r0 + r : (r0 + r) % a.G);
   const int2 who = a.info[id];
-  if ((who.x >> 1) == who.y) return;
-  // a lane has 4 columns (D = 128), 2 (64) or 1
+  // (a tile that no CTA began -- a wait that expired -- has any number here)
+  if (who.x < 0 || (who.x >> 1) >= who.y || who.y >= a.ctas) return;
+  // A lane has 4 columns (D = 128), 2 (64) or 1.  Partial results are taken 32 at a time: their maxima and sums by a lane
+  // each, then their outputs eight loads at a time -- one after the other, each would cost a trip to L2 (25 of them: 17 us).
   constexpr int E = D >= 64 ? D / 32 : 1;
-  const int col = lane * E;
+  const int col = lane * E, first = who.x >> 1, n = who.y - first + 1;
+  // all CTAs but the first begin their run inside the tile
+  auto part_of = [&](int i) { return a.part + ((long long)(first + i) * 2 + (i == 0 ? (who.x & 1) : 0)) * part_floats(PR, D); };
   float m = -INFINITY, l = 0.f, x[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) x[e] = 0.f;
-  for (int c = who.x >> 1; c <= who.y; ++c) {
-    // all CTAs but the first begin their run inside the tile
-    const float* part = a.part + ((long long)c * 2 + (c == (who.x >> 1) ? (who.x & 1) : 0)) * S::PART;
-    const float pm = part[R * D + r], pl = part[R * D + R + r];
-    const float top = fmaxf(m, pm), base = top == -INFINITY ? 0.f : top;
-    const float f = exp2f(m - base), pf = exp2f(pm - base);
+  for (int i0 = 0; i0 < n; i0 += 32) {
+    const bool has = i0 + lane < n;
+    const float* mine = part_of(has ? i0 + lane : i0);
+    const float pm = has ? mine[PR * D + r] : -INFINITY, pl = has ? mine[PR * (D + 1) + r] : 0.f;
+    const float top = fmaxf(m, warp_max(pm)), base = top == -INFINITY ? 0.f : top;
+    const float f = exp2f(m - base), w = exp2f(pm - base);
     m = top;
-    l = l * f + pl * pf;
-    if (col < D) {
+    l = l * f + warp_sum(pl * w);
 #pragma unroll
-      for (int e = 0; e < E; ++e) { const float y = part[r * D + col + e]; x[e] = x[e] * f + (pf != 0.f ? y * pf : 0.f); }
+    for (int e = 0; e < E; ++e) x[e] *= f;
+    const int k = min(32, n - i0);
+    for (int j0 = 0; j0 < k; j0 += 8) {
+      float y[8][E];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float* src = part_of(min(i0 + j0 + j, n - 1)) + r * D + (col < D ? col : 0);
+        if constexpr (E == 4) *reinterpret_cast<float4*>(y[j]) = *reinterpret_cast<const float4*>(src);
+        else if constexpr (E == 2) *reinterpret_cast<float2*>(y[j]) = *reinterpret_cast<const float2*>(src);
+        else y[j][0] = *src;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float wj = __shfl_sync(0xffffffffu, w, j0 + j);
+        if (wj != 0.f && j0 + j < k)
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[e] = fmaf(y[j][e], wj, x[e]);
+      }
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;

@@ -10,9 +10,10 @@ constexpr int kSMs = 148;
 
 // What a call of these sizes needs, and its launches.
 struct AttnPlan {
-  int ctas, tile_rows, tiles, combine_rows;   // tiles: that could be
+  int ctas, tile_rows, tiles, combine_rows, split;   // tiles: that could be
   size_t part_bytes, info_bytes;
 };
+constexpr int kWholeTileChunks = 6;           // tiles of at most so many chunks get a CTA each
 // Rows of a tile: as few as hold all rows of a key head, 64 at most.
 inline int tile_rows_of(bool paged, int rows) { return paged || rows <= 16 ? 16 : (rows <= 32 ? 32 : 64); }
 
@@ -28,10 +29,12 @@ int plan_one(const AttnArgs& a, AttnPlan* p) {
   if (tiles > 0x7fffffffLL) return fail(BPD_E_SHAPE, "batch * nodes * heads out of range");
   p->tiles = (int)tiles;
   const long long chunks = (PAGED ? std::min(a.select, a.ppr) + 1 : a.ppr) + ceil_div(a.T, kChunk);
-  p->ctas = (int)std::min<long long>(tiles * chunks, (long long)kSMs * S::CTAS_PER_SM);
+  const long long slots = (long long)kSMs * S::CTAS_PER_SM;
+  p->split = chunks > kWholeTileChunks;
+  p->ctas = (int)(p->split ? std::min(tiles * chunks, slots) : tiles);
   p->combine_rows = std::min(S::R, PAGED ? a.G : a.T * a.G);
-  p->part_bytes = (((size_t)p->ctas * 2 * S::PART * 4) + 255) / 256 * 256;
-  p->info_bytes = ((size_t)p->tiles * sizeof(int2) + 255) / 256 * 256;
+  p->part_bytes = p->split ? (((size_t)p->ctas * 2 * part_floats(p->combine_rows, D) * 4) + 255) / 256 * 256 : 0;
+  p->info_bytes = p->split ? ((size_t)p->tiles * sizeof(int2) + 255) / 256 * 256 : 256;
   return BPD_OK;
 }
 
@@ -41,8 +44,10 @@ int launch_one(const AttnArgs& a, const AttnPlan& p, cudaStream_t st) {
   int rc = ensure_smem_limit(reinterpret_cast<const void*>(tree_attention_kernel<CT, D, WR, PAGED>), S::SMEM);
   if (rc) return rc;
   BPD_CUDA(launch_k(tree_attention_kernel<CT, D, WR, PAGED>, dim3(p.ctas), dim3(kThreads), S::SMEM, st, false, a));
-  BPD_CUDA(launch_k(combine_kernel<CT, D, WR, PAGED>, dim3(p.tiles, ceil_div(p.combine_rows, 4)), dim3(kThreads), 0, st, true, a));
-  g_launches += 2;
+  ++g_launches;
+  if (!p.split) return BPD_OK;
+  BPD_CUDA(launch_k(combine_kernel<CT, D, PAGED>, dim3(p.tiles, ceil_div(p.combine_rows, 4)), dim3(kThreads), 0, st, true, a, p.tile_rows));
+  ++g_launches;
   return BPD_OK;
 }
 

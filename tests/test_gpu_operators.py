@@ -97,6 +97,7 @@ TREES = [
     ([300, 64], 33, 2, 2, 128, "random", [33, 1]), ([700, 5], 64, 4, 2, 64, "random", [64, 50]), ([90], 65, 3, 1, 16, "random", None),
     ([129], 200, 2, 1, 64, "random", None), ([20], 256, 1, 1, 32, "chain", None), ([64], 100, 2, 2, 128, "star", None),
     ([2500, 1, 640, 64], 3, 16, 1, 128, "random", [3, 1, 2, 3]), ([40] * 130, 2, 2, 1, 16, "chain", None),
+    ([1500], 1, 1, 1, 64, "chain", None), ([1500, 30], 3, 1, 1, 128, "chain", None), ([900], 5, 3, 1, 16, "random", None), ([2000, 1], 70, 4, 2, 128, "random", [70, 9]),
 ]
 
 
@@ -161,6 +162,7 @@ def test_values_of_device_arrays_are_not_trusted(bpd, dtype):
 PAGED = [
     ([0], 1, 1, 1, 16, 1, None), ([64], 1, 2, 2, 64, 1, None), ([63], 2, 4, 2, 64, 3, None), ([1000, 130], 3, 8, 2, 128, 4, [3, 2]),
     ([700, 64, 65, 5], 2, 20, 1, 64, 5, [2, 0, 1, 2]), ([2000], 1, 40, 2, 32, 7, None), ([5000], 4, 4, 4, 16, 30, None), ([640], 70, 2, 1, 64, 2, [70]),
+    ([2000, 700], 1, 1, 1, 64, 9, None), ([1500], 2, 3, 1, 128, 8, None),
 ]
 
 

@@ -125,7 +125,7 @@ def test_commit_weights_and_eviction_refuse(b):
 
 def test_scratch_grows_with_what_needs_it(b):
     n = b.lib.bpd_op_tree_attention_scratch_bytes(_cache(b), 4, 4)
-    assert 0 < n < b.lib.bpd_op_tree_attention_scratch_bytes(_cache(b, batch=64), 64, 4)
+    assert 0 < n < b.lib.bpd_op_tree_attention_scratch_bytes(_cache(b, batch=640, pages_per_row=50), 64, 4)
     assert b.lib.bpd_op_tree_attention_scratch_bytes(_cache(b, head_dim=7), 4, 4) == 0
     assert b.lib.bpd_op_cache_evict_scratch_bytes(_cache(b), 10 ** 9) == b.lib.bpd_op_cache_evict_scratch_bytes(_cache(b), 320)
 
@@ -144,7 +144,7 @@ def test_binding_refuses_tensors(b):
 
 def test_binding_takes_rows_one_stride_apart(b):
     import torch
-    cpu, f32 = torch.device("cpu"), torch.float32
+    cpu, f32 = -1, torch.float32
     fused = torch.zeros(3, 5, 400)
     part = fused[..., 128:256].unflatten(2, (2, 64))
     assert b._expect_rows(part, "x", (3, 5, 2, 64), f32, cpu) == (part.data_ptr(), 400)
@@ -165,6 +165,8 @@ def test_binding_takes_rows_one_stride_apart(b):
 # every unit of every tile falls to exactly one CTA, and the CTAs from a tile's first to its last are those that have units of it
 WORK = r"""
 #include <cstdio>
+#include <initializer_list>
+
 #include "cache_index.hpp"
 using namespace bpd::tree;
 int main() {
