@@ -419,6 +419,12 @@ int bpd_op_page_attention(const bpd_cache* cache, const float* means, const void
                           const int32_t* n_nodes, int select, float scale, void* scratch, size_t scratch_bytes, void* out,
                           float* lse, int32_t* pages, void* cuda_stream);
 
+/* What the operators on a paged cache cannot report as they only enqueue work:
+ * whether a bounded wait inside one of their kernels has expired on the current
+ * device since this was last asked (BPD_E_TIMEOUT; never seen outside of broken
+ * hardware or a debugger).  Synchronises the stream. */
+int bpd_op_status(void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -96,6 +96,7 @@ _SIGS = {
     "bpd_op_page_attention_scratch_bytes": (_sz, [_vp, _i, _i, _i]),
     "bpd_op_page_attention": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i64, _i64, _vp, _vp, _vp, _i, C.c_float, _vp, _sz, _vp, _vp, _vp,
                                    _vp]),
+    "bpd_op_status": (_i, [_vp]),
     "bpd_op_linear": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _vp, _sz, _vp, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
@@ -598,3 +599,9 @@ def bpd_op_page_means(k_pool, page_table, lens_from, lens, means):
     mp = _expect(means, "means", (pool[0], b, per_row, pool[3], pool[4]), torch.float32, device)
     _enqueue(device, lib.bpd_op_page_means, C.byref(c), _expect(lens_from, "lens_from", (b,), torch.int32, device),
              _expect(lens, "lens", (b,), torch.int32, device), mp)
+
+
+def bpd_op_status():
+    """Raises BpdError (BPD_E_TIMEOUT) if a bounded wait in a kernel of the operators above has expired on the current device since
+    the last call.  Synchronises the current stream."""
+    _check(lib.bpd_op_status(_stream()))

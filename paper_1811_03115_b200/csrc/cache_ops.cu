@@ -260,4 +260,11 @@ int bpd_op_cache_evict(const bpd_cache* cache, const int32_t* lens, const int32_
   return BPD_OK;
 }
 
+int bpd_op_status(void* cuda_stream) {
+  int expired = 0;
+  const int rc = take_wait_expired(&expired, (cudaStream_t)cuda_stream);
+  if (rc) return rc;
+  return expired ? fail(BPD_E_TIMEOUT, "a bounded wait of an operator's kernel expired; outputs enqueued since the last call are not valid") : BPD_OK;
+}
+
 }  // extern "C"

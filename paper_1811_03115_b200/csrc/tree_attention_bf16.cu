@@ -2,10 +2,76 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "tree_attention_tc.cuh"
+#include "tc_host.hpp"
 #include "tree_host.hpp"
 
 namespace bpd {
 namespace tree {
-BPD_TREE_INSTANTIATE(bf16)
+
+// Calls whose work is cut into runs go to the 5th-generation tensor cores where the head width is one of theirs; tiles are
+// then 128 rows.
+template <int D, bool PAGED>
+int plan_tc(const AttnArgs& a, AttnPlan* p) {
+  const long long per_head = PAGED ? ceil_div(a.G, kTcRows) : ceil_div(a.T * a.G, kTcRows);
+  const long long tiles = (long long)a.B * a.Hkv * per_head * (PAGED ? a.T : 1);
+  p->tc = 1;
+  p->tile_rows = kTcRows;
+  p->tiles = (int)tiles;
+  p->ctas = (int)std::min<long long>(tiles * max_chunks<PAGED>(a), (long long)kSMs * TcShape<D>::CTAS_PER_SM);
+  p->combine_rows = std::min(kTcRows, PAGED ? a.G : a.T * a.G);
+  scratch_of(D, p);
+  return BPD_OK;
+}
+
+// A bf16 matrix [rows, cols], boxes of 64 x 64, 128-byte swizzle.
+static int map_of(const void* ptr, long long rows, long long cols, long long ld, CUtensorMap* out) {
+  return tc::make_map_3d(ptr, 2, 1, 0, (uint64_t)rows, (uint64_t)cols, (uint64_t)ld, 64, kChunk, true, out);
+}
+
+template <int D, bool PAGED>
+int launch_tc(const AttnArgs& a, const AttnPlan& p, cudaStream_t st) {
+  using S = TcShape<D>;
+  TcMaps maps;
+  const long long width = (long long)a.Hkv * D;
+  int rc;
+  if ((rc = map_of(a.k_pool, (long long)a.n_pages * kPagePos, width, width, &maps.kp)) || (rc = map_of(a.v_pool, (long long)a.n_pages * kPagePos, width, width, &maps.vp)) ||
+      (rc = map_of(a.k_new, (long long)a.B * a.T, width, a.kv_stride, &maps.kn)) || (rc = map_of(a.v_new, (long long)a.B * a.T, width, a.kv_stride, &maps.vn)))
+    return rc;
+  if ((rc = ensure_smem_limit(reinterpret_cast<const void*>(tree_attention_tc_kernel<D, PAGED>), S::SMEM))) return rc;
+  BPD_CUDA(launch_k(tree_attention_tc_kernel<D, PAGED>, dim3(p.ctas), dim3(kTcThreads), S::SMEM, st, false, a, maps));
+  ++g_launches;
+  return launch_combine<bf16, D, PAGED>(a, p, st);
+}
+
+template <> int plan_attention<bf16>(const AttnArgs& a, bool paged, int D, AttnPlan* plan) {
+  BPD_TREE_BY_DIM({
+    int rc = by_rows<bf16, DD>(a, paged, [&](auto wr, auto pg) { return plan_one<bf16, DD, decltype(wr)::value, decltype(pg)::value>(a, plan); });
+    if constexpr (DD >= 64) {
+      if (!rc && plan->split) rc = paged ? plan_tc<DD, true>(a, plan) : plan_tc<DD, false>(a, plan);
+    }
+    return rc;
+  })
+}
+template <> int launch_attention<bf16>(const AttnArgs& a, bool paged, int D, const AttnPlan& plan, cudaStream_t st) {
+  BPD_TREE_BY_DIM({
+    if constexpr (DD >= 64) {
+      if (plan.tc) return paged ? launch_tc<DD, true>(a, plan, st) : launch_tc<DD, false>(a, plan, st);
+    }
+    return by_rows<bf16, DD>(a, paged, [&](auto wr, auto pg) { return launch_one<bf16, DD, decltype(wr)::value, decltype(pg)::value>(a, plan, st); });
+  })
+}
+
+int take_wait_expired(int* expired, cudaStream_t st) {
+  const int zero = 0;
+  BPD_CUDA(cudaMemcpyFromSymbolAsync(expired, g_wait_expired, sizeof(int), 0, cudaMemcpyDeviceToHost, st));
+  BPD_CUDA(cudaStreamSynchronize(st));
+  if (*expired) {
+    BPD_CUDA(cudaMemcpyToSymbolAsync(g_wait_expired, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, st));
+    BPD_CUDA(cudaStreamSynchronize(st));
+  }
+  return BPD_OK;
+}
+
 }  // namespace tree
 }  // namespace bpd

@@ -1,0 +1,428 @@
+// The tree attention of tree_attention.cuh on the 5th-generation tensor cores: bf16 caches with heads of 64 or 128, in calls
+// whose work is cut into runs of chunks.
+//
+// A tile is 128 query rows of a key head (fewer use fewer of the lanes).  Per chunk of 64 keys: S = Q K^T (tcgen05.mma, both
+// operands in shared memory) into tensor memory; a thread per row takes its 64 scores, and puts the weights back where the
+// scores were, as two bf16 planes; O += P V (P from tensor memory, V from shared memory as TMA brought it, keys outermost).
+// The running maximum a row is scaled by lags behind: O is rescaled only when the maximum has grown by more than 2^8, which
+// fp32 sums and bf16 planes carry without loss.
+//
+// Warps 0-3: softmax (lane = row), epilogue; warp 4: TMA; warp 5: MMA and tensor memory.  Two CTAs share an SM: one's softmax
+// runs under the other's products and loads.  Keys and values come page by page as TMA tiles (64 keys x 64 columns, 128-byte
+// swizzle); what lies behind a sequence's last key in its open page, or behind its last node in the tree's chunk, comes along
+// and is masked, its values zeroed in shared memory (0 times NaN is not 0).
+//
+// Every wait is bounded; on expiry the CTA notes it (see bpd_op_status), waits (bounded) for its copies and products in
+// flight, frees its tensor memory and returns.
+#pragma once
+#include "gemm_tc.cuh"
+#include "tree_attention.cuh"
+
+namespace bpd {
+namespace tree {
+
+constexpr int kTcThreads = 192, kTcRows = 128;
+
+template <int D>
+struct TcShape {
+  static constexpr int STAGES = D == 128 ? 2 : 4;
+  static constexpr int PANELS = D / 64;                       // of 64 columns
+  static constexpr int PANEL = kChunk * 128;                  // bytes of a panel of keys or values
+  static constexpr int Q_PANEL = kTcRows * 128;
+  static constexpr int Q_BYTES = PANELS * Q_PANEL, KV_BYTES = PANELS * PANEL;
+  static constexpr int SMEM = 1024 + Q_BYTES + 2 * STAGES * KV_BYTES;
+  static constexpr int TMEM_COLS = 256;                       // scores / weights of two chunks (64 columns each), outputs (D)
+  static constexpr int CTAS_PER_SM = 2;
+};
+
+// A wait of some operator's kernel has expired on this device since it was last asked (see bpd_op_status).
+static __device__ int g_wait_expired;
+
+__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* dead) {
+  if (tc::mbar_try_wait(bar, parity)) return true;
+  const unsigned long long t0 = clock64();
+  for (;;) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (tc::mbar_try_wait(bar, parity)) return true;
+    if (*dead) return false;
+    if ((unsigned long long)(clock64() - t0) > tc::kSpinCycles) {
+      *dead = 1;
+      return false;
+    }
+  }
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// The same answer in every lane.
+__device__ __forceinline__ bool wait_bar_warp(uint32_t bar, uint32_t parity, volatile int* dead) { return __all_sync(0xffffffffu, wait_bar(bar, parity, dead)); }
+
+#define BPD_TMEM_32(op, X)                                                                                            \
+  op(X[0]), op(X[1]), op(X[2]), op(X[3]), op(X[4]), op(X[5]), op(X[6]), op(X[7]), op(X[8]), op(X[9]), op(X[10]),      \
+      op(X[11]), op(X[12]), op(X[13]), op(X[14]), op(X[15]), op(X[16]), op(X[17]), op(X[18]), op(X[19]), op(X[20]),   \
+      op(X[21]), op(X[22]), op(X[23]), op(X[24]), op(X[25]), op(X[26]), op(X[27]), op(X[28]), op(X[29]), op(X[30]),   \
+      op(X[31])
+// 32 consecutive columns of this thread's lane; complete after tmem_wait_ld.
+__device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
+#define BPD_OUT(x) "=r"(x)
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
+      "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : BPD_TMEM_32(BPD_OUT, r) : "r"(at) : "memory");
+#undef BPD_OUT
+}
+__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) {
+#define BPD_IN(x) "r"(x)
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+      "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::BPD_TMEM_32(BPD_IN, r), "r"(at) : "memory");
+#undef BPD_IN
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// D += A B with A (128 rows, 16 bf16 of K in 8 columns) in tensor memory.
+__device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Values as the product's B operand: N (columns) is the contiguous dimension.  Rows of 64 columns (128 bytes, swizzled) are
+// keys, eight of them 1024 bytes apart from the next eight; the next 64 columns lie a panel further.
+__device__ __forceinline__ uint64_t value_desc(uint32_t saddr, int panel_bytes) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3ffff) >> 4);
+  d |= (uint64_t)(panel_bytes >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// A box of a map's only matrix.
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst), "l"(map),
+               "r"(bar), "r"(x), "r"(y), "r"(0) : "memory");
+}
+
+// kp, vp: the pools as [n_pages * 64][Hkv * D]; kn, vn: the drafted nodes' rows.
+struct TcMaps { CUtensorMap kp, vp, kn, vn; };
+
+template <int D, bool PAGED>
+__global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ TcMaps maps) {
+  using S = TcShape<D>;
+  constexpr int KS = S::STAGES;
+  pdl_launch_dependents();
+  extern __shared__ uint8_t tt_smem[];
+  const uint32_t base = (s_addr(tt_smem) + 1023u) & ~1023u;        // swizzled tiles need 1024-byte alignment
+  uint8_t* gen = tt_smem + (base - s_addr(tt_smem));
+  const uint32_t q_s = base, k_s = q_s + S::Q_BYTES, v_s = k_s + KS * S::KV_BYTES;
+  __shared__ __align__(8) unsigned long long s_bar[4 * KS + 7];
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_dead, s_odd, s_keys[KS], s_parents[kMaxNodes];
+  const uint32_t bars = s_addr(s_bar);
+  auto k_full = [&](int s) { return bars + 8 * s; };
+  auto k_empty = [&](int s) { return bars + 8 * (KS + s); };
+  auto v_full = [&](int s) { return bars + 8 * (2 * KS + s); };
+  auto v_empty = [&](int s) { return bars + 8 * (3 * KS + s); };
+  auto s_full = [&](int s) { return bars + 8 * (4 * KS + s); };
+  auto p_ready = [&](int s) { return bars + 8 * (4 * KS + 2 + s); };
+  const uint32_t pv_done = bars + 8 * (4 * KS + 4), q_ready = bars + 8 * (4 * KS + 5), rows_bar = bars + 8 * (4 * KS + 6);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  clear_dead_rows<bf16>(a, D);
+  Walk<PAGED> w(a, kTcRows);
+  if (!w.begin()) return;                                          // (the same answer in every warp)
+  if (tid == 0) {
+    for (int s = 0; s < KS; ++s) { tc::mbar_init(k_full(s), 1); tc::mbar_init(k_empty(s), 1); tc::mbar_init(v_full(s), 1); tc::mbar_init(v_empty(s), 1); }
+    for (int s = 0; s < 2; ++s) { tc::mbar_init(s_full(s), 1); tc::mbar_init(p_ready(s), 4); }
+    tc::mbar_init(pv_done, 1);
+    tc::mbar_init(q_ready, 4);
+    tc::mbar_init(rows_bar, 4);
+    s_dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 5) tc::tmem_alloc(s_addr(&s_tmem), S::TMEM_COLS);
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = s_tmem, o_tmem = tmem + 128;
+  volatile int* dead = &s_dead;
+
+  if (warp == 4) {
+    // ---- loads
+    if (lane == 0) {
+      int n = 0;
+      bool ok = true;
+      do {
+        const int cached = w.cache_chunks();
+        int page = w.page_of(w.c_begin);
+        for (int c = w.c_begin; c < w.c_end && ok; ++c, ++n) {
+          const int st = n % KS, ph = (n / KS) & 1;
+          const int next_page = c + 1 < w.c_end ? w.page_of(c + 1) : -1;
+          const bool node = c >= cached;
+          // (a page that is not there: some page comes instead, all of it masked)
+          const int y = node ? w.b * a.T + (c - cached) * kChunk : max(page, 0) * kPagePos;
+          if (!(ok = wait_bar(k_empty(st), ph ^ 1, dead))) break;
+          tc::mbar_expect_tx(k_full(st), S::KV_BYTES);
+#pragma unroll
+          for (int p = 0; p < S::PANELS; ++p) load_box(k_s + st * S::KV_BYTES + p * S::PANEL, node ? &maps.kn : &maps.kp, k_full(st), w.tl.h * D + p * 64, y);
+          if (!(ok = wait_bar(v_empty(st), ph ^ 1, dead))) { tc::mbar_wait(k_full(st), ph); break; }
+          s_keys[st] = w.keys_of(c, page);                         // (read until the values before have been used)
+          tc::mbar_expect_tx(v_full(st), S::KV_BYTES);
+#pragma unroll
+          for (int p = 0; p < S::PANELS; ++p) load_box(v_s + st * S::KV_BYTES + p * S::PANEL, node ? &maps.vn : &maps.vp, v_full(st), w.tl.h * D + p * 64, y);
+          page = next_page;
+        }
+      } while (ok && w.next());
+      // after an expired wait: copies in flight land before the shared memory goes
+      if (!ok || *dead)
+        for (int i = max(0, n - KS); i < n; ++i) { tc::mbar_wait(k_full(i % KS), (i / KS) & 1); tc::mbar_wait(v_full(i % KS), (i / KS) & 1); }
+    }
+  } else if (warp == 5) {
+    // ---- products
+    if (lane == 0) {
+      const uint32_t id_s = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kChunk >> 3) << 17) | ((uint32_t)(kTcRows >> 4) << 24);
+      const uint32_t id_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTcRows >> 4) << 24);
+      auto scores = [&](int n) {
+        const int st = n % KS;
+        if (!wait_bar(k_full(st), (n / KS) & 1, dead)) return false;
+        tc::tc_fence_after();
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+          tc::umma_f16(tmem + (n & 1) * 64, tc::smem_desc_sw128(q_s + k / 4 * S::Q_PANEL + (k % 4) * 32),
+                       tc::smem_desc_sw128(k_s + st * S::KV_BYTES + k / 4 * S::PANEL + (k % 4) * 32), id_s, k > 0);
+        tc::umma_commit(s_full(n & 1));
+        tc::umma_commit(k_empty(st));
+        return true;
+      };
+      int n = 0, tile = 0;
+      bool ok = true;
+      do {
+        ok = wait_bar(q_ready, tile & 1, dead);
+        tc::tc_fence_after();
+        const int count = w.c_end - w.c_begin;
+        if (ok) ok = scores(n);
+        for (int i = 0; i < count && ok; ++i, ++n) {
+          const int st = n % KS;
+          // (the next chunk's scores take the place of weights whose product was issued before them)
+          if (i + 1 < count && !(ok = scores(n + 1))) break;
+          if (!(ok = wait_bar(p_ready(n & 1), (n >> 1) & 1, dead)) || !(ok = wait_bar(v_full(st), (n / KS) & 1, dead))) break;
+          tc::tc_fence_after();
+#pragma unroll
+          for (int plane = 0; plane < 2; ++plane)
+#pragma unroll
+            for (int k = 0; k < kChunk / 16; ++k)
+              umma_f16_ts(o_tmem, tmem + (n & 1) * 64 + plane * 32 + k * 8, value_desc(v_s + st * S::KV_BYTES + k * 2048, S::PANEL), id_o,
+                          i > 0 || plane > 0 || k > 0);
+          tc::umma_commit(v_empty(st));
+          tc::umma_commit(pv_done);
+        }
+        ++tile;
+      } while (ok && w.next());
+      if (!ok) {
+        // nothing may write tensor memory once it is freed: pv_done's next phase ends when all products have
+        tc::umma_commit(pv_done);
+        const unsigned long long t0 = clock64();
+        while (clock64() - t0 < 1000000ull) {}
+      }
+    }
+  } else {
+    // ---- softmax: a thread per row
+    const uint32_t my = (uint32_t)(warp * 32) << 16;
+    int n = 0, lines_of = -1, met = 0;
+    bool ok = true;
+    // the four warps meet
+    auto meet = [&] {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(rows_bar);
+      return wait_bar_warp(rows_bar, met++ & 1, dead);
+    };
+    do {
+      const int rows = w.rows(), r = tid, cached = w.cache_chunks(), count = w.c_end - w.c_begin, b = w.b;
+      const bool active = warp * 32 < rows;
+      // queries into swizzled shared memory; the outputs of the tile before have been read
+      for (int i = tid; i < ((rows + 31) & ~31) * (D / 8); i += 128) {
+        const int row = i / (D / 8), piece = i % (D / 8);
+        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+        if (row < rows)
+          x = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(a.q) + ((long long)b * a.T + w.node_of(row)) * a.q_stride + w.head_of(row) * D + piece * 8);
+        *reinterpret_cast<uint4*>(gen + piece / 8 * S::Q_PANEL + row * 128 + ((piece % 8) ^ (row & 7)) * 16) = x;
+      }
+      fence_async_shared();
+      tc::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_ready);
+      const bool tree = w.c_end > cached;
+      if (tree) {
+        if (!(ok = meet())) break;
+        if (lines_of != b) {
+          for (int i = tid; i < w.sq.nodes; i += 128) s_parents[i] = a.parents[(long long)b * a.T + i];
+          lines_of = b;
+        }
+        if (tid == 0) s_odd = 0;
+        if (!(ok = meet())) break;
+      }
+      float m = -INFINITY, l = 0.f;                                // m: what the weights are scaled by, a maximum of the past
+      for (int i = 0; i < count; ++i, ++n) {
+        const int c = w.c_begin + i, st = n % KS, sb = n & 1;
+        const bool node = c >= cached;
+        if (!(ok = wait_bar_warp(s_full(sb), (n >> 1) & 1, dead))) break;
+        tc::tc_fence_after();
+        if (!(ok = wait_bar_warp(v_full(st), (n / KS) & 1, dead))) break;
+        const int n_keys = s_keys[st];
+        const bool partial = n_keys < kChunk || node;
+        // keys behind the last: their values become 0; in the tree's chunk so do values that are no finite numbers, see below
+        if (partial) {
+          uint8_t* vb = gen + (v_s - base) + st * S::KV_BYTES;
+          for (int j = tid; j < kChunk * (D / 8); j += 128) {
+            const int key = j / (D / 8), piece = j % (D / 8);
+            uint4* at = reinterpret_cast<uint4*>(vb + piece / 8 * S::PANEL + key * 128 + ((piece % 8) ^ (key & 7)) * 16);
+            if (key >= n_keys) {
+              *at = make_uint4(0u, 0u, 0u, 0u);
+            } else if (node) {
+              uint4 v = *at;
+              uint32_t* x = reinterpret_cast<uint32_t*>(&v);
+              bool odd = false;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if ((x[e] & 0x7f80u) == 0x7f80u) { x[e] &= 0xffff0000u; odd = true; }
+                if ((x[e] & 0x7f800000u) == 0x7f800000u) { x[e] &= 0x0000ffffu; odd = true; }
+              }
+              if (odd) { *at = v; s_odd = 1; }
+            }
+          }
+          fence_async_shared();
+        }
+        if (active) {
+          uint32_t s[64];
+          {
+            uint32_t (&s0)[32] = *reinterpret_cast<uint32_t (*)[32]>(&s[0]);
+            uint32_t (&s1)[32] = *reinterpret_cast<uint32_t (*)[32]>(&s[32]);
+            tmem_ld32(tmem + my + sb * 64, s0);
+            tmem_ld32(tmem + my + sb * 64 + 32, s1);
+            tmem_wait_ld();
+          }
+          if (partial) {
+            unsigned long long see = n_keys >= 64 ? ~0ull : (1ull << n_keys) - 1;
+            if (node) see &= r < rows ? line_bits(s_parents, w.node_of(r), c - cached) : 0ull;
+#pragma unroll
+            for (int j = 0; j < 64; ++j) if (!((see >> j) & 1)) s[j] = 0xff800000u;
+          }
+          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int j = 0; j < 64; ++j) top[j & 3] = fmaxf(top[j & 3], __uint_as_float(s[j]));
+          const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
+          // (a row that has seen nothing keeps a maximum of -inf; its weights are taken against 0 and are 0)
+          if (__any_sync(0xffffffffu, now > m + 8.f)) {
+            const float higher = fmaxf(m, now), f = higher == -INFINITY ? 1.f : exp2_fast(m - higher);
+            m = higher;
+            l *= f;
+            if (i > 0) {
+              if (!(ok = wait_bar_warp(pv_done, (n - 1) & 1, dead))) break;
+              tc::tc_fence_after();
+#pragma unroll
+              for (int d = 0; d < D; d += 32) {
+                uint32_t x[32];
+                tmem_ld32(o_tmem + my + d, x);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
+                tmem_st32(o_tmem + my + d, x);
+              }
+              tmem_wait_st();
+            }
+          }
+          const float ref = m == -INFINITY ? 0.f : m;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          uint32_t hi[32], lo[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            const float p0 = exp2_fast(fmaf(__uint_as_float(s[2 * j]), a.scale_log2, -ref)), p1 = exp2_fast(fmaf(__uint_as_float(s[2 * j + 1]), a.scale_log2, -ref));
+            sum[j & 3] += p0 + p1;
+            // the high plane is the weight cut off behind 8 bits, the low plane what is left, rounded
+            hi[j] = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
+            const __nv_bfloat162 rest = __floats2bfloat162_rn(p0 - __uint_as_float(__float_as_uint(p0) & 0xffff0000u),
+                                                              p1 - __uint_as_float(__float_as_uint(p1) & 0xffff0000u));
+            lo[j] = *reinterpret_cast<const uint32_t*>(&rest);
+          }
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          tmem_st32(tmem + my + sb * 64, hi);
+          tmem_st32(tmem + my + sb * 64 + 32, lo);
+          tmem_wait_st();
+        }
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_ready(sb));
+      }
+      if (!ok) break;
+      // ---- the tile's result
+      if (!(ok = wait_bar_warp(pv_done, (n - 1) & 1, dead))) break;
+      tc::tc_fence_after();
+      if (tree && !(ok = meet())) break;
+      const bool whole = w.whole(), odd = tree && s_odd;
+      if (active) {
+        const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+        const long long at = r < rows ? w.out_row(r) : 0;
+        float* part = a.part + ((long long)blockIdx.x * 2 + (a.split ? w.slot : 0)) * part_floats(a.part_rows, D);
+#pragma unroll
+        for (int d = 0; d < D; d += 32) {
+          uint32_t x[32];
+          tmem_ld32(o_tmem + my + d, x);
+          tmem_wait_ld();
+          if (r < rows) {
+            // Values that were no finite numbers: a row that sees one has no finite output there, whatever its weight.
+            if (odd) {
+              const int node0 = max(0, w.c_begin - cached) * kChunk, node1 = (w.c_end - cached) * kChunk;
+              for (int t = w.node_of(r); t >= 0; t = parent_of(s_parents[t], t)) {
+                if (t < node0 || t >= node1) continue;
+                const bf16* v = reinterpret_cast<const bf16*>(a.v_new) + ((long long)b * a.T + t) * a.kv_stride + w.tl.h * D + d;
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                  const float y = __bfloat162float(v[e]);
+                  if (!(fabsf(y) <= 3.402823466e38f)) x[e] = __float_as_uint(__uint_as_float(x[e]) + y);
+                }
+              }
+            }
+            if (whole) {
+              bf16* o = reinterpret_cast<bf16*>(a.out) + at * D + d;
+#pragma unroll
+              for (int e = 0; e < 32; e += 8) {
+                uint32_t y[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const __nv_bfloat162 v2 = __floats2bfloat162_rn(__uint_as_float(x[e + 2 * k]) * inv, __uint_as_float(x[e + 2 * k + 1]) * inv);
+                  y[k] = *reinterpret_cast<const uint32_t*>(&v2);
+                }
+                *reinterpret_cast<uint4*>(o + e) = make_uint4(y[0], y[1], y[2], y[3]);
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(part + (long long)r * D + d + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+            }
+          }
+        }
+        if (r < rows) {
+          if (whole && a.lse) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945f;
+          if (!whole) { part[(long long)a.part_rows * D + r] = m; part[(long long)a.part_rows * (D + 1) + r] = l; }
+        }
+      }
+      if (a.split && w.c_begin == 0 && tid == 0) a.info[w.tl.id] = make_int2(blockIdx.x * 2 + w.slot, w.last_cta);
+    } while (w.next());
+  }
+  __syncwarp();
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  if (warp == 5) tc::tmem_dealloc(tmem, S::TMEM_COLS);
+  if (tid == 0 && s_dead) g_wait_expired = 1;
+}
+
+}  // namespace tree
+}  // namespace bpd

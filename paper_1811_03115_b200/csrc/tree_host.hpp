@@ -10,7 +10,7 @@ constexpr int kSMs = 148;
 
 // What a call of these sizes needs, and its launches.
 struct AttnPlan {
-  int ctas, tile_rows, tiles, combine_rows, split;   // tiles: that could be
+  int ctas, tile_rows, tiles, combine_rows, split, tc;   // tiles: that could be
   size_t part_bytes, info_bytes;
 };
 constexpr int kWholeTileChunks = 6;           // tiles of at most so many chunks get a CTA each
@@ -20,21 +20,36 @@ inline int tile_rows_of(bool paged, int rows) { return paged || rows <= 16 ? 16 
 template <typename CT> int plan_attention(const AttnArgs& a, bool paged, int D, AttnPlan* plan);
 template <typename CT> int launch_attention(const AttnArgs& a, bool paged, int D, const AttnPlan& plan, cudaStream_t st);
 
+// The most chunks of a tile.
+template <bool PAGED>
+long long max_chunks(const AttnArgs& a) { return (PAGED ? std::min(a.select, a.ppr) + 1 : a.ppr) + ceil_div(a.T, kChunk); }
+
+inline void scratch_of(int D, AttnPlan* p) {
+  const size_t part = (size_t)p->ctas * 2 * part_floats(p->combine_rows, D) * 4;
+  p->part_bytes = p->split ? (part + 255) / 256 * 256 : 0;
+  p->info_bytes = p->split ? ((size_t)p->tiles * sizeof(int2) + 255) / 256 * 256 : 256;
+}
+
 template <typename CT, int D, int WR, bool PAGED>
 int plan_one(const AttnArgs& a, AttnPlan* p) {
   using S = Shape<CT, D, WR>;
   p->tile_rows = S::R;
+  p->tc = 0;
   const long long per_head = PAGED ? ceil_div(a.G, S::R) : ceil_div(a.T * a.G, S::R);
   const long long tiles = (long long)a.B * a.Hkv * per_head * (PAGED ? a.T : 1);
   if (tiles > 0x7fffffffLL) return fail(BPD_E_SHAPE, "batch * nodes * heads out of range");
   p->tiles = (int)tiles;
-  const long long chunks = (PAGED ? std::min(a.select, a.ppr) + 1 : a.ppr) + ceil_div(a.T, kChunk);
-  const long long slots = (long long)kSMs * S::CTAS_PER_SM;
-  p->split = chunks > kWholeTileChunks;
-  p->ctas = (int)(p->split ? std::min(tiles * chunks, slots) : tiles);
+  p->split = max_chunks<PAGED>(a) > kWholeTileChunks;
+  p->ctas = (int)(p->split ? std::min<long long>(tiles * max_chunks<PAGED>(a), (long long)kSMs * S::CTAS_PER_SM) : tiles);
   p->combine_rows = std::min(S::R, PAGED ? a.G : a.T * a.G);
-  p->part_bytes = p->split ? (((size_t)p->ctas * 2 * part_floats(p->combine_rows, D) * 4) + 255) / 256 * 256 : 0;
-  p->info_bytes = p->split ? ((size_t)p->tiles * sizeof(int2) + 255) / 256 * 256 : 256;
+  scratch_of(D, p);
+  return BPD_OK;
+}
+
+template <typename CT, int D, bool PAGED>
+int launch_combine(const AttnArgs& a, const AttnPlan& p, cudaStream_t st) {
+  BPD_CUDA(launch_k(combine_kernel<CT, D, PAGED>, dim3(p.tiles, ceil_div(p.combine_rows, 4)), dim3(kThreads), 0, st, true, a, p.tile_rows));
+  ++g_launches;
   return BPD_OK;
 }
 
@@ -45,10 +60,7 @@ int launch_one(const AttnArgs& a, const AttnPlan& p, cudaStream_t st) {
   if (rc) return rc;
   BPD_CUDA(launch_k(tree_attention_kernel<CT, D, WR, PAGED>, dim3(p.ctas), dim3(kThreads), S::SMEM, st, false, a));
   ++g_launches;
-  if (!p.split) return BPD_OK;
-  BPD_CUDA(launch_k(combine_kernel<CT, D, PAGED>, dim3(p.tiles, ceil_div(p.combine_rows, 4)), dim3(kThreads), 0, st, true, a, p.tile_rows));
-  ++g_launches;
-  return BPD_OK;
+  return p.split ? launch_combine<CT, D, PAGED>(a, p, st) : BPD_OK;
 }
 
 template <typename CT, int D, typename F>
@@ -61,21 +73,16 @@ int by_rows(const AttnArgs& a, bool paged, F&& f) {
   }
 }
 
-#define BPD_TREE_BY_DIM(call)                \
-  switch (D) {                               \
-    case 16: { constexpr int DD = 16; call } \
-    case 32: { constexpr int DD = 32; call } \
-    case 64: { constexpr int DD = 64; call } \
-    default: { constexpr int DD = 128; call }\
+#define BPD_TREE_BY_DIM(...)                \
+  switch (D) {                                      \
+    case 16: { constexpr int DD = 16; __VA_ARGS__ }        \
+    case 32: { constexpr int DD = 32; __VA_ARGS__ }        \
+    case 64: { constexpr int DD = 64; __VA_ARGS__ }        \
+    default: { constexpr int DD = 128; __VA_ARGS__ }       \
   }
 
-#define BPD_TREE_INSTANTIATE(CT)                                                                          \
-  template <> int plan_attention<CT>(const AttnArgs& a, bool paged, int D, AttnPlan* plan) {              \
-    BPD_TREE_BY_DIM(return (by_rows<CT, DD>(a, paged, [&](auto wr, auto pg) { return plan_one<CT, DD, decltype(wr)::value, decltype(pg)::value>(a, plan); }));) \
-  }                                                                                                       \
-  template <> int launch_attention<CT>(const AttnArgs& a, bool paged, int D, const AttnPlan& plan, cudaStream_t st) { \
-    BPD_TREE_BY_DIM(return (by_rows<CT, DD>(a, paged, [&](auto wr, auto pg) { return launch_one<CT, DD, decltype(wr)::value, decltype(pg)::value>(a, plan, st); }));) \
-  }
+// Whether a wait of an operator's kernel has expired on the current device since it was last asked.
+int take_wait_expired(int* expired, cudaStream_t st);
 
 }  // namespace tree
 }  // namespace bpd

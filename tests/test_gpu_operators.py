@@ -128,9 +128,10 @@ def test_tree_attention_of_slices_of_one_projection(bpd, dtype):
 
 
 # siblings hold infinities and NaN: only their own lines may see them
-@pytest.mark.parametrize("dtype,dim,nodes", [("bf16", 64, 9), ("fp32", 64, 9), ("bf16", 128, 40), ("fp32", 16, 20)])
-def test_values_that_are_no_numbers_stay_in_their_line(bpd, dtype, dim, nodes):
-    c = Case(5, [10, 0], nodes, 2, 1, dim, dtype, tree="star")
+@pytest.mark.parametrize("dtype,dim,nodes,length", [("bf16", 64, 9, 10), ("fp32", 64, 9, 10), ("bf16", 128, 40, 0), ("fp32", 16, 20, 10), ("bf16", 64, 9, 500),
+                                                    ("bf16", 128, 70, 1000), ("fp32", 32, 70, 600)])
+def test_values_that_are_no_numbers_stay_in_their_line(bpd, dtype, dim, nodes, length):
+    c = Case(5, [length, 0], nodes, 2, 1, dim, dtype, tree="star")
     c.parents[:, 3] = 1
     c.parents[:, 4] = 3
     bad = [2, 5, nodes - 1]
