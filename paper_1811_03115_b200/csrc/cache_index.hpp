@@ -39,10 +39,36 @@ BPD_HD SeqWork paged_work(int len, int nodes, int select, int kv_heads, int grou
   return w;
 }
 
-// `units` units over `ctas` <= units CTAs, each a contiguous run of at least one: the first unit of CTA i, and the CTA that
-// has unit u.
-BPD_HD long long first_unit(long long i, long long units, long long ctas) { return i * units / ctas; }
-BPD_HD int cta_of_unit(long long u, long long units, long long ctas) { return (int)(((u + 1) * ctas - 1) / units); }
+// `units` units over `ctas` <= units CTAs, each a contiguous run: the first units % ctas of them one unit longer.  (Divisions
+// of 64-bit numbers take the device ten times as long as those of 32 bits, and a small call's CTAs wait for them.)
+struct Runs {
+  long long units;
+  int ctas, extra;           // extra: CTAs with size + 1 units
+  long long size;
+};
+BPD_HD Runs runs_of(long long units, int max_ctas) {
+  Runs r;
+  r.units = units;
+  r.ctas = units < max_ctas ? (int)units : max_ctas;
+  if (units <= 0) { r.size = 0; r.extra = 0; return r; }
+  if (units <= 0x7fffffffLL) {
+    const unsigned size = (unsigned)units / (unsigned)r.ctas;
+    r.size = size;
+    r.extra = (int)((unsigned)units - size * (unsigned)r.ctas);
+  } else {
+    r.size = units / r.ctas;
+    r.extra = (int)(units - r.size * r.ctas);
+  }
+  return r;
+}
+// The first unit of CTA i, and the CTA that has unit u.
+BPD_HD long long first_unit(const Runs& r, int i) { return i * r.size + (i < r.extra ? i : r.extra); }
+BPD_HD int cta_of_unit(const Runs& r, long long u) {
+  const long long longer = r.extra * (r.size + 1);
+  if (r.units <= 0x7fffffffLL)
+    return u < longer ? (int)((unsigned)u / (unsigned)(r.size + 1)) : r.extra + (int)((unsigned)(u - longer) / (unsigned)r.size);
+  return u < longer ? (int)(u / (r.size + 1)) : r.extra + (int)((u - longer) / r.size);
+}
 
 // Row of the pool ([n_pages, 64] rows) that holds position pos, -1 if the table has no page of the pool for it.
 BPD_HD long long pool_row(int page, int n_pages, int pos) {

@@ -18,6 +18,7 @@
 // core's own additions truncate).
 #pragma once
 #include "attention.cuh"
+#include "gemm_tc.cuh"
 #include "cache_index.hpp"
 
 namespace bpd {
@@ -30,6 +31,7 @@ using attn::s_addr;
 using attn::split3_pair;
 
 constexpr int kThreads = 128;
+constexpr int kPagesAhead = 64;   // pages looked up at a time
 constexpr int kChunk = kPagePos;
 
 struct AttnArgs {
@@ -48,8 +50,39 @@ struct AttnArgs {
   int2* info;                                  // per tile: 2 * first CTA that has units of it + the slot of its partial result; last CTA
 };
 
-// Shared-memory layout of a chunk's rows.  bf16: 16-byte pieces, XOR-swizzled so that eight consecutive rows' same piece
-// lies in eight different 16-byte columns of the banks; fp32: padded rows (see attention.cuh).
+// ---------------------------------------------------------------- waits and loads
+// A wait of some operator's kernel has expired on this device since it was last asked (see bpd_op_status).
+static __device__ int g_wait_expired;
+
+__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* dead) {
+  if (tc::mbar_try_wait(bar, parity)) return true;
+  const unsigned long long t0 = clock64();
+  for (;;) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (tc::mbar_try_wait(bar, parity)) return true;
+    if (*dead) return false;
+    if ((unsigned long long)(clock64() - t0) > tc::kSpinCycles) {
+      *dead = 1;
+      return false;
+    }
+  }
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// A box of a map's only matrix.
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst), "l"(map),
+               "r"(bar), "r"(x), "r"(y), "r"(0) : "memory");
+}
+
+// kp, vp: the pools as [n_pages * 64][Hkv * D]; kn, vn: the drafted nodes' rows.
+struct TcMaps { CUtensorMap kp, vp, kn, vn; };
+
+// ---------------------------------------------------------------- layouts
+// Shared-memory layout of a chunk's rows.  bf16: panels of up to 64 columns, their 16-byte pieces XOR-swizzled so that eight
+// consecutive rows' same piece lies in eight different 16-byte columns of the banks (for 64 columns: what TMA's 128-byte
+// swizzle writes); fp32: padded rows (see attention.cuh).
 template <typename CT, int D>
 struct Rows {
   static constexpr bool F32 = sizeof(CT) == 4;
@@ -60,8 +93,8 @@ struct Rows {
   static constexpr int V_BYTES = F32 ? kChunk * VP * 4 : kChunk * D * 2;
   static constexpr int STAGE = K_BYTES + V_BYTES;
   __device__ __forceinline__ static uint32_t swz(int row, int piece) {
-    constexpr int PER_LINE = PIECES >= 8 ? 1 : 8 / PIECES, MASK = PIECES >= 8 ? 7 : PIECES - 1;
-    return (uint32_t)(row * PIECES + (piece ^ ((row / PER_LINE) & MASK))) * 16u;
+    constexpr int ACROSS = PIECES >= 8 ? 8 : PIECES, PER_LINE = 8 / ACROSS;      // pieces of a panel's row, rows of 128 bytes
+    return (uint32_t)(piece / ACROSS * kChunk * ACROSS + row * ACROSS + ((piece % ACROSS) ^ ((row / PER_LINE) % ACROSS))) * 16u;
   }
   __device__ __forceinline__ static uint32_t k_at(int row, int piece) { return F32 ? (uint32_t)(row * KP + piece * 4) * 4u : swz(row, piece); }
   __device__ __forceinline__ static uint32_t v_at(int row, int piece) { return F32 ? (uint32_t)(row * VP + piece * 4) * 4u : swz(row, piece); }
@@ -78,7 +111,7 @@ struct Shape {
   static constexpr int MERGE = WK * R * MP * 4;
   static constexpr int STAGES = F32 ? (D >= 128 ? 2 : 3) : (D >= 128 ? 3 : 4);
   static constexpr int RING = STAGES * Rows<CT, D>::STAGE;
-  static constexpr int SMEM = Q_BYTES + (RING > MERGE ? RING : MERGE);
+  static constexpr int SMEM = 1024 + Q_BYTES + (RING > MERGE ? RING : MERGE);   // (TMA's tiles begin at multiples of 1024)
   static constexpr int CTAS_PER_SM = F32 ? (D >= 128 ? 1 : 2) : (D >= 128 ? 2 : 3);
 };
 
@@ -148,7 +181,8 @@ template <bool PAGED>
 struct Walk {
   const AttnArgs& a;
   const int tile_rows;
-  long long units, ctas, u_begin, u, u_end, seq_first;
+  Runs runs;
+  long long u_begin, u, u_end, seq_first;
   int b;
   Seq sq;
   Tile tl;
@@ -182,11 +216,10 @@ struct Walk {
     for (int i = lane; i < a.B; i += 32) sum += units_of(i);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    units = sum;
-    ctas = min(units, (long long)gridDim.x);                // no CTA that shares a tile may be without a unit
-    if (blockIdx.x >= ctas) return false;
-    u = u_begin = first_unit(blockIdx.x, units, ctas);
-    u_end = first_unit(blockIdx.x + 1, units, ctas);
+    runs = runs_of(sum, (int)gridDim.x);                    // (no CTA that shares a tile may be without a unit)
+    if ((int)blockIdx.x >= runs.ctas) return false;
+    u = u_begin = first_unit(runs, blockIdx.x);
+    u_end = first_unit(runs, blockIdx.x + 1);
     long long before = 0;
     for (int b0 = 0;; b0 += 32) {
       const long long n = b0 + lane < a.B ? units_of(b0 + lane) : 0;
@@ -219,13 +252,14 @@ struct Walk {
     return true;
   }
   __device__ __forceinline__ void find() {
-    const int local = (int)((u - seq_first) / sq.w.chunks);
+    const long long into = u - seq_first;
+    const int local = into <= 0x7fffffffLL ? (int)((unsigned)into / (unsigned)sq.w.chunks) : (int)(into / sq.w.chunks);
     const long long tile_first = seq_first + (long long)local * sq.w.chunks;
     c_begin = (int)(u - tile_first);
     c_end = (int)min((long long)sq.w.chunks, u_end - tile_first);
     tl = tile_of<PAGED>(a, b, sq.nodes, local, tile_rows);
     slot = u == u_begin ? 0 : 1;                            // a CTA leaves at most two partial results: of its first tile, of its last
-    last_cta = c_begin == 0 && c_end < sq.w.chunks ? cta_of_unit(tile_first + sq.w.chunks - 1, units, ctas) : (int)blockIdx.x;
+    last_cta = c_begin == 0 && c_end < sq.w.chunks ? cta_of_unit(runs, tile_first + sq.w.chunks - 1) : (int)blockIdx.x;
   }
   __device__ __forceinline__ int rows() const { return PAGED ? min(tile_rows, a.G - tl.r0) : min(tile_rows, sq.nodes * a.G - tl.r0); }
   // node and head of row r of the tile, and its row of the output
@@ -270,19 +304,23 @@ __device__ __forceinline__ void clear_dead_rows(const AttnArgs& a, int D) {
   }
 }
 
-template <typename CT, int D, int WR, bool PAGED>
-__global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_constant__ AttnArgs a) {
+// TMA: pages come as TMA tiles (bf16, heads of 64 and 128), else by 16-byte asynchronous copies of every thread.  With the
+// copies, half of the loop's instructions were addresses; TMA's tensor maps cost the host a few microseconds a call, so small
+// calls do without.
+template <typename CT, int D, int WR, bool PAGED, bool TMA>
+__global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ TcMaps maps) {
   using S = Shape<CT, D, WR>;
   using L = Rows<CT, D>;
   pdl_launch_dependents();
   constexpr bool F32 = S::F32;
   constexpr int R = S::R, WK = S::WK, KW = S::KW, KT = D / 16, NT = KW / 8, DT = D / 8;
   extern __shared__ __align__(128) uint8_t ta_smem[];
-  __shared__ int s_keys[S::STAGES], s_parents[kMaxNodes];
+  __shared__ __align__(8) unsigned long long s_full[S::STAGES];
+  __shared__ int s_dead, s_keys[S::STAGES], s_pages[kPagesAhead], s_parents[kMaxNodes];
   __shared__ unsigned long long s_line[R][kMaxNodes / 64];
   __shared__ float s_m[WK][R], s_l[WK][R];
-  bf16* qs = reinterpret_cast<bf16*>(ta_smem);
-  uint8_t* ring = ta_smem + S::Q_BYTES;
+  uint8_t* ring = ta_smem + ((1024u - (s_addr(ta_smem) & 1023u)) & 1023u);
+  bf16* qs = reinterpret_cast<bf16*>(ring + (S::SMEM - 1024 - S::Q_BYTES));
   const uint32_t ring_s = s_addr(ring);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
   const int wr = warp % WR, wk = warp / WR;
@@ -291,42 +329,70 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
   Walk<PAGED> w(a, R);
   if (!w.begin()) return;
   int lines_of = -1;                                        // sequence whose parents are in shared memory
+  int n = 0;                                                // chunks so far
+  if (TMA) {
+    if (tid == 0) {
+      for (int s = 0; s < S::STAGES; ++s) tc::mbar_init(s_addr(&s_full[s]), 1);
+      s_dead = 0;
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+  }
 
   do {
     const int rows = w.rows(), b = w.b, cache_chunks = w.cache_chunks(), c_begin = w.c_begin, c_end = w.c_end;
-    auto page_of = [&](int c) { return w.page_of(c); };
-    auto keys_of = [&](int c, int page) { return w.keys_of(c, page); };
     auto node_of = [&](int r) { return w.node_of(r); };
     auto head_of = [&](int r) { return w.head_of(r); };
     const Tile& tl = w.tl;
     const Seq& sq = w.sq;
     const int tree_chunks = w.tree_chunks();
-    auto load = [&](int c, int page, int stage) {
-      const CT *k, *v;
-      long long step;
-      const int n = keys_of(c, page);
-      if (c >= cache_chunks) {
-        const long long at = ((long long)b * a.T + (c - cache_chunks) * kChunk) * a.kv_stride + tl.h * D;
-        k = reinterpret_cast<const CT*>(a.k_new) + at;
-        v = reinterpret_cast<const CT*>(a.v_new) + at;
-        step = a.kv_stride;
-      } else {
-        const long long at = ((long long)max(page, 0) * kPagePos * a.Hkv + tl.h) * D;
-        k = reinterpret_cast<const CT*>(a.k_pool) + at;
-        v = reinterpret_cast<const CT*>(a.v_pool) + at;
-        step = (long long)a.Hkv * D;
-      }
+    // Pages of the chunks from c0 on, and a barrier.
+    auto look_up = [&](int c0) {
+      for (int i = tid; i < kPagesAhead && c0 + i < c_end; i += kThreads) s_pages[i] = w.page_of(c0 + i);
+      __syncthreads();
+    };
+    auto load = [&](int c, int stage) {
+      const int page = s_pages[(c - c_begin) % kPagesAhead], n_keys = w.keys_of(c, page);
       const uint32_t ks = ring_s + stage * L::STAGE, vs = ks + L::K_BYTES;
-      constexpr int PER_PASS = kThreads / L::PIECES >= 1 ? kThreads / L::PIECES : 1;
-      const int piece = tid % L::PIECES;
+      const bool node = c >= cache_chunks;
+      if (tid == 0) s_keys[stage] = n_keys;                 // (read behind the barrier at the chunk's turn)
+      if constexpr (TMA) {
+        if (tid == 0) {
+          // (a page that is not there: some page comes instead, all of it masked)
+          const int y = node ? b * a.T + (c - cache_chunks) * kChunk : max(page, 0) * kPagePos;
+          const uint32_t bar = s_addr(&s_full[stage]);
+          tc::mbar_expect_tx(bar, L::STAGE);
 #pragma unroll
-      for (int r0 = 0; r0 < kChunk; r0 += PER_PASS) {
-        const int r = r0 + tid / L::PIECES;
+          for (int p = 0; p < D / 64; ++p) {
+            load_box(ks + p * kChunk * 128, node ? &maps.kn : &maps.kp, bar, tl.h * D + p * 64, y);
+            load_box(vs + p * kChunk * 128, node ? &maps.vn : &maps.vp, bar, tl.h * D + p * 64, y);
+          }
+        }
+        return;
+      }
+      const long long at = node ? ((long long)b * a.T + (c - cache_chunks) * kChunk) * a.kv_stride + tl.h * D : ((long long)max(page, 0) * kPagePos * a.Hkv + tl.h) * D;
+      const long long step = node ? a.kv_stride : (long long)a.Hkv * D;
+      constexpr int PER_PASS = kThreads / L::PIECES;
+      const int row = tid / L::PIECES, piece = tid % L::PIECES;
+      const CT* k = reinterpret_cast<const CT*>(node ? a.k_new : a.k_pool) + at + row * step + piece * L::PER;
+      const CT* v = reinterpret_cast<const CT*>(node ? a.v_new : a.v_pool) + at + row * step + piece * L::PER;
+      if (n_keys == kChunk) {
+#pragma unroll
+        for (int r0 = 0; r0 < kChunk; r0 += PER_PASS) {
+          cp_async16(ks + L::k_at(r0 + row, piece), k);
+          cp_async16(vs + L::v_at(r0 + row, piece), v);
+          k += PER_PASS * step;
+          v += PER_PASS * step;
+        }
+      } else {
         // rows behind the last key are filled with zeros: a weight of 0 times what lies there must be 0
-        const int bytes = r < n ? 16 : 0;
-        const long long at = r < n ? r * step + piece * L::PER : 0;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ks + L::k_at(r, piece)), "l"(k + at), "r"(bytes) : "memory");
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vs + L::v_at(r, piece)), "l"(v + at), "r"(bytes) : "memory");
+#pragma unroll
+        for (int r0 = 0; r0 < kChunk; r0 += PER_PASS) {
+          const bool there = r0 + row < n_keys;
+          const int bytes = there ? 16 : 0;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ks + L::k_at(r0 + row, piece)), "l"(there ? k + r0 * step : reinterpret_cast<const CT*>(a.k_pool)), "r"(bytes) : "memory");
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vs + L::v_at(r0 + row, piece)), "l"(there ? v + r0 * step : reinterpret_cast<const CT*>(a.v_pool)), "r"(bytes) : "memory");
+        }
       }
     };
 
@@ -374,35 +440,38 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
     for (int i = 0; i < DT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
     float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;   // maxima are of scores times scale_log2
 
-    // the ring: the number of keys of each chunk in it goes along (thread 0 writes, a barrier later all read)
-    int page_next = page_of(c_begin);                       // a table entry is fetched one chunk ahead of its rows
+    look_up(c_begin);
 #pragma unroll
     for (int s = 0; s < S::STAGES - 1; ++s) {
-      const int c = c_begin + s;
-      if (c < c_end) {
-        load(c, page_next, s);
-        if (tid == 0) s_keys[s] = keys_of(c, page_next);
-        page_next = page_of(c + 1);
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
+      if (c_begin + s < c_end) load(c_begin + s, (n + s) % S::STAGES);
+      if (!TMA) asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    int stage = 0;
-    for (int c = c_begin; c < c_end; ++c) {
-      asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 2) : "memory");
-      __syncthreads();                                      // the chunk is there, and the stage before it has been used
+    for (int c = c_begin; c < c_end; ++c, ++n) {
+      const int stage = n % S::STAGES;
+      if (!TMA) asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 2) : "memory");
+      __syncthreads();                                      // the stage before has been used (and, copied, the chunk is there)
       {
-        const int cn = c + S::STAGES - 1, sn = stage == 0 ? S::STAGES - 1 : stage - 1;
+        const int cn = c + S::STAGES - 1;
         if (cn < c_end) {
-          load(cn, page_next, sn);
-          if (tid == 0) s_keys[sn] = keys_of(cn, page_next);
-          page_next = page_of(cn + 1);
+          if ((cn - c_begin) % kPagesAhead == 0) look_up(cn);
+          load(cn, (n + S::STAGES - 1) % S::STAGES);
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (!TMA) asm volatile("cp.async.commit_group;" ::: "memory");
       }
       const uint8_t* kb = ring + stage * L::STAGE;
       const uint8_t* vb = kb + L::K_BYTES;
       const uint32_t ks = ring_s + stage * L::STAGE, vs = ks + L::K_BYTES;
       const int n_keys = s_keys[stage], key0 = wk * KW;
+      if constexpr (TMA) {
+        // (after an expired wait the rest runs on whatever is there: see bpd_op_status)
+        wait_bar(s_addr(&s_full[stage]), (n / S::STAGES) & 1, &s_dead);
+        if (n_keys < kChunk) {
+          for (int i = n_keys * L::PIECES + tid; i < kChunk * L::PIECES; i += kThreads)
+            *reinterpret_cast<uint4*>(const_cast<uint8_t*>(vb) + L::v_at(i / L::PIECES, i % L::PIECES)) = make_uint4(0u, 0u, 0u, 0u);
+          fence_async_shared();
+          __syncthreads();
+        }
+      }
 
       // scores of the warp's 16 rows and KW keys
       float s[NT][4];
@@ -572,11 +641,10 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
           }
         }
       }
-      stage = stage + 1 == S::STAGES ? 0 : stage + 1;
     }
 
     // join the warps that shared the rows
-    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (!TMA) asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();                                        // the ring has been used
     l0 += __shfl_xor_sync(0xffffffffu, l0, 1); l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
     l1 += __shfl_xor_sync(0xffffffffu, l1, 1); l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
@@ -620,17 +688,25 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
       }
     }
     if (!a.split) return;
+    if (TMA) fence_async_shared();                          // the ring's next contents come by TMA
     if (c_begin == 0 && tid == 0) a.info[tl.id] = make_int2(blockIdx.x * 2 + w.slot, w.last_cta);
     __syncthreads();                                        // the ring, the lines and the sums are free again
   } while (w.next());
+  if (TMA && tid == 0 && s_dead) g_wait_expired = 1;
 }
 
-// Joins the partial results of the tiles that more than one CTA worked on.  grid: (tiles that could be, R / 4), a warp per row.
-template <typename CT, int D, bool PAGED>
+// Joins the partial results of the tiles that more than one CTA worked on.  grid: (tiles that could be, rows / (4 / SHARE)):
+// SHARE (4 or 1) warps to a row, each of which takes 8 partial results at a time, all loads under way together -- one after the
+// other, each would cost a trip to L2.  A row's 33 partial results took a warp alone 4 us; where there are thousands of rows
+// they fill the device as it is, and warps that find nothing to do cost more (128 rows of 512 tiles: 75 us more).
+template <typename CT, int D, bool PAGED, int SHARE>
 __global__ void __launch_bounds__(kThreads) combine_kernel(const __grid_constant__ AttnArgs a, int tile_rows) {
-  const int R = tile_rows, PR = a.part_rows;
   pdl_wait();                                               // (every CTA: the launch after this one waits for this one alone)
-  const int id = blockIdx.x, r = blockIdx.y * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  // a lane has 4 columns (D = 128), 2 (64) or 1
+  constexpr int E = D >= 64 ? D / 32 : 1, WARPS = kThreads / 32, PER = 8;
+  __shared__ float s_m[WARPS], s_l[WARPS], s_x[SHARE > 1 ? WARPS : 1][32 * E];
+  const int R = tile_rows, PR = a.part_rows;
+  const int id = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = blockIdx.y * (WARPS / SHARE) + warp / SHARE;
   int b, h, t, r0;
   if (PAGED) {
     const int rt = ceil_div(a.G, R);
@@ -639,49 +715,68 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(const __grid_constant
     const int rt = ceil_div(a.T * a.G, R);
     r0 = id % rt * R; h = id / rt % a.Hkv; b = id / rt / a.Hkv; t = 0;
   }
+  const int2 who = a.info[id];
   const int nodes = a.nodes ? clamp_int(a.nodes[b], 0, a.T) : a.T;
   const int rows = PAGED ? (t < nodes ? a.G : 0) : nodes * a.G;
   if (r0 + r >= rows) return;
   const int node = PAGED ? t : (r0 + r) / a.G, head = h * a.G + (PAGED ? r0 + r : (r0 + r) % a.G);
-  const int2 who = a.info[id];
   // (a tile that no CTA began -- a wait that expired -- has any number here)
   if (who.x < 0 || (who.x >> 1) >= who.y || who.y >= a.ctas) return;
-  // A lane has 4 columns (D = 128), 2 (64) or 1.  Partial results are taken 32 at a time: their maxima and sums by a lane
-  // each, then their outputs eight loads at a time -- one after the other, each would cost a trip to L2 (25 of them: 17 us).
-  constexpr int E = D >= 64 ? D / 32 : 1;
   const int col = lane * E, first = who.x >> 1, n = who.y - first + 1;
   // all CTAs but the first begin their run inside the tile
   auto part_of = [&](int i) { return a.part + ((long long)(first + i) * 2 + (i == 0 ? (who.x & 1) : 0)) * part_floats(PR, D); };
   float m = -INFINITY, l = 0.f, x[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) x[e] = 0.f;
-  for (int i0 = 0; i0 < n; i0 += 32) {
-    const bool has = i0 + lane < n;
-    const float* mine = part_of(has ? i0 + lane : i0);
-    const float pm = has ? mine[PR * D + r] : -INFINITY, pl = has ? mine[PR * (D + 1) + r] : 0.f;
-    const float top = fmaxf(m, warp_max(pm)), base = top == -INFINITY ? 0.f : top;
-    const float f = exp2f(m - base), w = exp2f(pm - base);
+  for (int i0 = warp % SHARE * PER; i0 < n; i0 += SHARE * PER) {
+    float pm[PER], pl[PER], y[PER][E];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const bool has = i0 + j < n;
+      const float* src = part_of(has ? i0 + j : i0);
+      pm[j] = has ? src[PR * D + r] : -INFINITY;
+      pl[j] = src[PR * (D + 1) + r];
+      src += r * D + (col < D ? col : 0);
+      if constexpr (E == 4) *reinterpret_cast<float4*>(y[j]) = *reinterpret_cast<const float4*>(src);
+      else if constexpr (E == 2) *reinterpret_cast<float2*>(y[j]) = *reinterpret_cast<const float2*>(src);
+      else y[j][0] = *src;
+    }
+    float top = m;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) top = fmaxf(top, pm[j]);
+    const float base = top == -INFINITY ? 0.f : top, f = exp2f(m - base);
     m = top;
-    l = l * f + warp_sum(pl * w);
+    l *= f;
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] *= f;
-    const int k = min(32, n - i0);
-    for (int j0 = 0; j0 < k; j0 += 8) {
-      float y[8][E];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float* src = part_of(min(i0 + j0 + j, n - 1)) + r * D + (col < D ? col : 0);
-        if constexpr (E == 4) *reinterpret_cast<float4*>(y[j]) = *reinterpret_cast<const float4*>(src);
-        else if constexpr (E == 2) *reinterpret_cast<float2*>(y[j]) = *reinterpret_cast<const float2*>(src);
-        else y[j][0] = *src;
-      }
+    for (int j = 0; j < PER; ++j) {
+      const bool has = i0 + j < n;                          // (selected here, not branched on: the loads stay side by side)
+      const float w = exp2f(pm[j] - base);
+      l = fmaf(has ? pl[j] : 0.f, w, l);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float wj = __shfl_sync(0xffffffffu, w, j0 + j);
-        if (wj != 0.f && j0 + j < k)
+      for (int e = 0; e < E; ++e) x[e] = fmaf(has ? y[j][e] : 0.f, w, x[e]);
+    }
+  }
+  if constexpr (SHARE > 1) {
+    if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
 #pragma unroll
-          for (int e = 0; e < E; ++e) x[e] = fmaf(y[j][e], wj, x[e]);
-      }
+    for (int e = 0; e < E; ++e) s_x[warp][lane * E + e] = x[e];
+    __syncthreads();
+    if (warp > 0) return;
+    m = s_m[0];
+#pragma unroll
+    for (int w = 1; w < WARPS; ++w) m = fmaxf(m, s_m[w]);
+    const float base = m == -INFINITY ? 0.f : m;
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      const float f = exp2f(s_m[w] - base);
+      l = fmaf(s_l[w], f, l);
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = fmaf(s_x[w][lane * E + e], f, x[e]);
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;

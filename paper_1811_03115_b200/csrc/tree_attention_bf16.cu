@@ -9,8 +9,9 @@
 namespace bpd {
 namespace tree {
 
-// Calls whose work is cut into runs go to the 5th-generation tensor cores where the head width is one of theirs; tiles are
-// then 128 rows.
+// Calls whose work is cut into runs, heads of 64 and 128: with more than 32 rows to a key head the tiles are 128 rows and go
+// to the 5th-generation tensor cores.  With fewer, a tile's products are short and its softmax is one warp's, and the kernel
+// whose four warps share the keys is the faster one.  SWEEP
 template <int D, bool PAGED>
 int plan_tc(const AttnArgs& a, AttnPlan* p) {
   const long long per_head = PAGED ? ceil_div(a.G, kTcRows) : ceil_div(a.T * a.G, kTcRows);
@@ -29,16 +30,21 @@ static int map_of(const void* ptr, long long rows, long long cols, long long ld,
   return tc::make_map_3d(ptr, 2, 1, 0, (uint64_t)rows, (uint64_t)cols, (uint64_t)ld, 64, kChunk, true, out);
 }
 
-template <int D, bool PAGED>
-int launch_tc(const AttnArgs& a, const AttnPlan& p, cudaStream_t st) {
-  using S = TcShape<D>;
-  TcMaps maps;
-  const long long width = (long long)a.Hkv * D;
+template <int D>
+int maps_of(const AttnArgs& a, TcMaps* maps) {
+  const long long width = (long long)a.Hkv * D, positions = (long long)a.n_pages * kPagePos, nodes = (long long)a.B * a.T;
   int rc;
-  if ((rc = map_of(a.k_pool, (long long)a.n_pages * kPagePos, width, width, &maps.kp)) || (rc = map_of(a.v_pool, (long long)a.n_pages * kPagePos, width, width, &maps.vp)) ||
-      (rc = map_of(a.k_new, (long long)a.B * a.T, width, a.kv_stride, &maps.kn)) || (rc = map_of(a.v_new, (long long)a.B * a.T, width, a.kv_stride, &maps.vn)))
+  if ((rc = map_of(a.k_pool, positions, width, width, &maps->kp)) || (rc = map_of(a.v_pool, positions, width, width, &maps->vp)) ||
+      (rc = map_of(a.k_new, nodes, width, a.kv_stride, &maps->kn)) || (rc = map_of(a.v_new, nodes, width, a.kv_stride, &maps->vn)))
     return rc;
-  if ((rc = ensure_smem_limit(reinterpret_cast<const void*>(tree_attention_tc_kernel<D, PAGED>), S::SMEM))) return rc;
+  return BPD_OK;
+}
+
+template <int D, bool PAGED>
+int launch_tc(const AttnArgs& a, const TcMaps& maps, const AttnPlan& p, cudaStream_t st) {
+  using S = TcShape<D>;
+  int rc = ensure_smem_limit(reinterpret_cast<const void*>(tree_attention_tc_kernel<D, PAGED>), S::SMEM);
+  if (rc) return rc;
   BPD_CUDA(launch_k(tree_attention_tc_kernel<D, PAGED>, dim3(p.ctas), dim3(kTcThreads), S::SMEM, st, false, a, maps));
   ++g_launches;
   return launch_combine<bf16, D, PAGED>(a, p, st);
@@ -48,17 +54,27 @@ template <> int plan_attention<bf16>(const AttnArgs& a, bool paged, int D, AttnP
   BPD_TREE_BY_DIM({
     int rc = by_rows<bf16, DD>(a, paged, [&](auto wr, auto pg) { return plan_one<bf16, DD, decltype(wr)::value, decltype(pg)::value>(a, plan); });
     if constexpr (DD >= 64) {
-      if (!rc && plan->split) rc = paged ? plan_tc<DD, true>(a, plan) : plan_tc<DD, false>(a, plan);
+      if (!rc && plan->split && (paged ? a.G : a.T * a.G) > 32) rc = paged ? plan_tc<DD, true>(a, plan) : plan_tc<DD, false>(a, plan);
     }
     return rc;
   })
 }
 template <> int launch_attention<bf16>(const AttnArgs& a, bool paged, int D, const AttnPlan& plan, cudaStream_t st) {
+  TcMaps maps;
   BPD_TREE_BY_DIM({
     if constexpr (DD >= 64) {
-      if (plan.tc) return paged ? launch_tc<DD, true>(a, plan, st) : launch_tc<DD, false>(a, plan, st);
+      if (plan.split) {
+        const int rc = maps_of<DD>(a, &maps);
+        if (rc) return rc;
+        if (plan.tc) return paged ? launch_tc<DD, true>(a, maps, plan, st) : launch_tc<DD, false>(a, maps, plan, st);
+        return by_rows<bf16, DD>(a, paged, [&](auto wr, auto pg) {
+          if constexpr (decltype(wr)::value <= 2) return launch_one<bf16, DD, decltype(wr)::value, decltype(pg)::value, true>(a, maps, plan, st);
+          else return fail(BPD_E_UNSUPPORTED, "no kernel for %d rows", a.T * a.G);   // (more than 32 rows: plan.tc)
+        });
+      }
     }
-    return by_rows<bf16, DD>(a, paged, [&](auto wr, auto pg) { return launch_one<bf16, DD, decltype(wr)::value, decltype(pg)::value>(a, plan, st); });
+    memset(&maps, 0, sizeof(maps));
+    return by_rows<bf16, DD>(a, paged, [&](auto wr, auto pg) { return launch_one<bf16, DD, decltype(wr)::value, decltype(pg)::value, false>(a, maps, plan, st); });
   })
 }
 

@@ -15,7 +15,6 @@
 // Every wait is bounded; on expiry the CTA notes it (see bpd_op_status), waits (bounded) for its copies and products in
 // flight, frees its tensor memory and returns.
 #pragma once
-#include "gemm_tc.cuh"
 #include "tree_attention.cuh"
 
 namespace bpd {
@@ -35,25 +34,6 @@ struct TcShape {
   static constexpr int CTAS_PER_SM = 2;
 };
 
-// A wait of some operator's kernel has expired on this device since it was last asked (see bpd_op_status).
-static __device__ int g_wait_expired;
-
-__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* dead) {
-  if (tc::mbar_try_wait(bar, parity)) return true;
-  const unsigned long long t0 = clock64();
-  for (;;) {
-#pragma unroll 1
-    for (int i = 0; i < 64; ++i)
-      if (tc::mbar_try_wait(bar, parity)) return true;
-    if (*dead) return false;
-    if ((unsigned long long)(clock64() - t0) > tc::kSpinCycles) {
-      *dead = 1;
-      return false;
-    }
-  }
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // The same answer in every lane.
 __device__ __forceinline__ bool wait_bar_warp(uint32_t bar, uint32_t parity, volatile int* dead) { return __all_sync(0xffffffffu, wait_bar(bar, parity, dead)); }
 
@@ -105,15 +85,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
-// A box of a map's only matrix.
-__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst), "l"(map),
-               "r"(bar), "r"(x), "r"(y), "r"(0) : "memory");
-}
-
-// kp, vp: the pools as [n_pages * 64][Hkv * D]; kn, vn: the drafted nodes' rows.
-struct TcMaps { CUtensorMap kp, vp, kn, vn; };
-
 template <int D, bool PAGED>
 __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ TcMaps maps) {
   using S = TcShape<D>;
@@ -156,35 +127,42 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
   volatile int* dead = &s_dead;
 
   if (warp == 4) {
-    // ---- loads
-    if (lane == 0) {
-      int n = 0;
-      bool ok = true;
-      do {
-        const int cached = w.cache_chunks();
-        int page = w.page_of(w.c_begin);
-        for (int c = w.c_begin; c < w.c_end && ok; ++c, ++n) {
-          const int st = n % KS, ph = (n / KS) & 1;
-          const int next_page = c + 1 < w.c_end ? w.page_of(c + 1) : -1;
+    // ---- loads: a lane each looks up the pages of 32 chunks, the first lane issues
+    int n = 0;
+    bool ok = true;
+    do {
+      const int cached = w.cache_chunks();
+      int pages = -1;
+      for (int c = w.c_begin; c < w.c_end && ok; ++c, ++n) {
+        const int ahead = (c - w.c_begin) % 32;
+        if (ahead == 0) pages = c + lane < w.c_end ? w.page_of(c + lane) : -1;
+        const int page = __shfl_sync(0xffffffffu, pages, ahead);
+        const int st = n % KS, ph = (n / KS) & 1;
+        if (lane == 0) {
           const bool node = c >= cached;
           // (a page that is not there: some page comes instead, all of it masked)
           const int y = node ? w.b * a.T + (c - cached) * kChunk : max(page, 0) * kPagePos;
-          if (!(ok = wait_bar(k_empty(st), ph ^ 1, dead))) break;
-          tc::mbar_expect_tx(k_full(st), S::KV_BYTES);
+          if ((ok = wait_bar(k_empty(st), ph ^ 1, dead))) {
+            tc::mbar_expect_tx(k_full(st), S::KV_BYTES);
 #pragma unroll
-          for (int p = 0; p < S::PANELS; ++p) load_box(k_s + st * S::KV_BYTES + p * S::PANEL, node ? &maps.kn : &maps.kp, k_full(st), w.tl.h * D + p * 64, y);
-          if (!(ok = wait_bar(v_empty(st), ph ^ 1, dead))) { tc::mbar_wait(k_full(st), ph); break; }
-          s_keys[st] = w.keys_of(c, page);                         // (read until the values before have been used)
-          tc::mbar_expect_tx(v_full(st), S::KV_BYTES);
+            for (int p = 0; p < S::PANELS; ++p) load_box(k_s + st * S::KV_BYTES + p * S::PANEL, node ? &maps.kn : &maps.kp, k_full(st), w.tl.h * D + p * 64, y);
+            if ((ok = wait_bar(v_empty(st), ph ^ 1, dead))) {
+              s_keys[st] = w.keys_of(c, page);                     // (read until the values before have been used)
+              tc::mbar_expect_tx(v_full(st), S::KV_BYTES);
 #pragma unroll
-          for (int p = 0; p < S::PANELS; ++p) load_box(v_s + st * S::KV_BYTES + p * S::PANEL, node ? &maps.vn : &maps.vp, v_full(st), w.tl.h * D + p * 64, y);
-          page = next_page;
+              for (int p = 0; p < S::PANELS; ++p) load_box(v_s + st * S::KV_BYTES + p * S::PANEL, node ? &maps.vn : &maps.vp, v_full(st), w.tl.h * D + p * 64, y);
+            } else {
+              tc::mbar_wait(k_full(st), ph);
+            }
+          }
         }
-      } while (ok && w.next());
-      // after an expired wait: copies in flight land before the shared memory goes
-      if (!ok || *dead)
-        for (int i = max(0, n - KS); i < n; ++i) { tc::mbar_wait(k_full(i % KS), (i / KS) & 1); tc::mbar_wait(v_full(i % KS), (i / KS) & 1); }
-    }
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (!ok) break;
+      }
+    } while (ok && w.next());
+    // after an expired wait: copies in flight land before the shared memory goes
+    if (lane == 0 && (!ok || *dead))
+      for (int i = max(0, n - KS); i < n; ++i) { tc::mbar_wait(k_full(i % KS), (i / KS) & 1); tc::mbar_wait(v_full(i % KS), (i / KS) & 1); }
   } else if (warp == 5) {
     // ---- products
     if (lane == 0) {

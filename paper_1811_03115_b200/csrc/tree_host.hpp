@@ -48,17 +48,21 @@ int plan_one(const AttnArgs& a, AttnPlan* p) {
 
 template <typename CT, int D, bool PAGED>
 int launch_combine(const AttnArgs& a, const AttnPlan& p, cudaStream_t st) {
-  BPD_CUDA(launch_k(combine_kernel<CT, D, PAGED>, dim3(p.tiles, ceil_div(p.combine_rows, 4)), dim3(kThreads), 0, st, true, a, p.tile_rows));
+  if ((long long)p.tiles * p.combine_rows <= 16 * kSMs)
+    BPD_CUDA(launch_k(combine_kernel<CT, D, PAGED, 4>, dim3(p.tiles, p.combine_rows), dim3(kThreads), 0, st, true, a, p.tile_rows));
+  else
+    BPD_CUDA(launch_k(combine_kernel<CT, D, PAGED, 1>, dim3(p.tiles, ceil_div(p.combine_rows, 4)), dim3(kThreads), 0, st, true, a, p.tile_rows));
   ++g_launches;
   return BPD_OK;
 }
 
-template <typename CT, int D, int WR, bool PAGED>
-int launch_one(const AttnArgs& a, const AttnPlan& p, cudaStream_t st) {
+template <typename CT, int D, int WR, bool PAGED, bool TMA>
+int launch_one(const AttnArgs& a, const TcMaps& maps, const AttnPlan& p, cudaStream_t st) {
   using S = Shape<CT, D, WR>;
-  int rc = ensure_smem_limit(reinterpret_cast<const void*>(tree_attention_kernel<CT, D, WR, PAGED>), S::SMEM);
+  const auto kernel = tree_attention_kernel<CT, D, WR, PAGED, TMA>;
+  int rc = ensure_smem_limit(reinterpret_cast<const void*>(kernel), S::SMEM);
   if (rc) return rc;
-  BPD_CUDA(launch_k(tree_attention_kernel<CT, D, WR, PAGED>, dim3(p.ctas), dim3(kThreads), S::SMEM, st, false, a));
+  BPD_CUDA(launch_k(kernel, dim3(p.ctas), dim3(kThreads), S::SMEM, st, false, a, maps));
   ++g_launches;
   return p.split ? launch_combine<CT, D, PAGED>(a, p, st) : BPD_OK;
 }

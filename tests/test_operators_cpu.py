@@ -170,16 +170,17 @@ WORK = r"""
 #include "cache_index.hpp"
 using namespace bpd::tree;
 int main() {
-  const long long sizes[] = {1, 2, 3, 40, 147, 148, 149, 443, 444, 445, 1000, 99991, 5000000000LL};
+  const long long sizes[] = {1, 2, 3, 40, 147, 148, 149, 443, 444, 445, 1000, 99991, 2147483647LL, 2147483648LL, 5000000000LL};
   for (long long units : sizes)
-    for (long long grid : {1LL, 2LL, 60LL, 148LL, 444LL}) {
-      const long long ctas = units < grid ? units : grid;
-      if (first_unit(0, units, ctas) != 0 || first_unit(ctas, units, ctas) != units) return 1;
-      for (long long i = 0; i < ctas; ++i) {
-        const long long a = first_unit(i, units, ctas), z = first_unit(i + 1, units, ctas);
-        if (a >= z || cta_of_unit(a, units, ctas) != i || cta_of_unit(z - 1, units, ctas) != i) return 2;
+    for (int grid : {1, 2, 60, 148, 444}) {
+      const Runs r = runs_of(units, grid);
+      if (r.ctas != (units < grid ? units : grid) || first_unit(r, 0) != 0 || first_unit(r, r.ctas) != units) return 1;
+      for (int i = 0; i < r.ctas; ++i) {
+        const long long a = first_unit(r, i), z = first_unit(r, i + 1);
+        if (a >= z || z - a > units / r.ctas + 1 || cta_of_unit(r, a) != i || cta_of_unit(r, z - 1) != i) return 2;
       }
     }
+  if (runs_of(0, 5).ctas != 0) return 9;
   for (int len : {0, 1, 63, 64, 65, 1000})
     for (int nodes : {0, 1, 63, 64, 65, 256})
       for (int group : {1, 3, 16, 17})
