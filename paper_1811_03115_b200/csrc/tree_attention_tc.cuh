@@ -24,12 +24,15 @@ constexpr int kTcThreads = 192, kTcRows = 128;
 
 template <int D>
 struct TcShape {
-  static constexpr int STAGES = D == 128 ? 2 : 4;
+  // Stages of keys and of values.  A chunk's keys are used up as soon as its scores are there, a chunk ahead of their softmax;
+  // its values two softmaxes later.  So most of the room goes to the values (with two stages each and one order of issue,
+  // loads had one softmax of time, and a third of every chunk's 3400 cycles was spent waiting for them).
+  static constexpr int KK = D == 128 ? 1 : 2, KV = D == 128 ? 3 : 4;
   static constexpr int PANELS = D / 64;                       // of 64 columns
   static constexpr int PANEL = kChunk * 128;                  // bytes of a panel of keys or values
   static constexpr int Q_PANEL = kTcRows * 128;
   static constexpr int Q_BYTES = PANELS * Q_PANEL, KV_BYTES = PANELS * PANEL;
-  static constexpr int SMEM = 1024 + Q_BYTES + 2 * STAGES * KV_BYTES;
+  static constexpr int SMEM = 1024 + Q_BYTES + (KK + KV) * KV_BYTES;
   static constexpr int TMEM_COLS = 256;                       // scores / weights of two chunks (64 columns each), outputs (D)
   static constexpr int CTAS_PER_SM = 2;
 };
@@ -88,30 +91,31 @@ __device__ __forceinline__ float exp2_fast(float x) {
 template <int D, bool PAGED>
 __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ TcMaps maps) {
   using S = TcShape<D>;
-  constexpr int KS = S::STAGES;
+  constexpr int KK = S::KK, KV = S::KV;
   pdl_launch_dependents();
   extern __shared__ uint8_t tt_smem[];
   const uint32_t base = (s_addr(tt_smem) + 1023u) & ~1023u;        // swizzled tiles need 1024-byte alignment
   uint8_t* gen = tt_smem + (base - s_addr(tt_smem));
-  const uint32_t q_s = base, k_s = q_s + S::Q_BYTES, v_s = k_s + KS * S::KV_BYTES;
-  __shared__ __align__(8) unsigned long long s_bar[4 * KS + 7];
+  const uint32_t q_s = base, k_s = q_s + S::Q_BYTES, v_s = k_s + KK * S::KV_BYTES;
+  __shared__ __align__(8) unsigned long long s_bar[2 * (KK + KV) + 7];
   __shared__ uint32_t s_tmem;
-  __shared__ int s_dead, s_odd, s_keys[KS], s_parents[kMaxNodes];
+  __shared__ int s_dead, s_odd, s_keys[4], s_parents[kMaxNodes];
   const uint32_t bars = s_addr(s_bar);
-  auto k_full = [&](int s) { return bars + 8 * s; };
-  auto k_empty = [&](int s) { return bars + 8 * (KS + s); };
-  auto v_full = [&](int s) { return bars + 8 * (2 * KS + s); };
-  auto v_empty = [&](int s) { return bars + 8 * (3 * KS + s); };
-  auto s_full = [&](int s) { return bars + 8 * (4 * KS + s); };
-  auto p_ready = [&](int s) { return bars + 8 * (4 * KS + 2 + s); };
-  const uint32_t pv_done = bars + 8 * (4 * KS + 4), q_ready = bars + 8 * (4 * KS + 5), rows_bar = bars + 8 * (4 * KS + 6);
+  auto k_full = [&](int n) { return bars + 8 * (n % KK); };         // of chunk n (of the CTA's)
+  auto k_empty = [&](int n) { return bars + 8 * (KK + n % KK); };
+  auto v_full = [&](int n) { return bars + 8 * (2 * KK + n % KV); };
+  auto v_empty = [&](int n) { return bars + 8 * (2 * KK + KV + n % KV); };
+  auto s_full = [&](int s) { return bars + 8 * (2 * (KK + KV) + s); };
+  auto p_ready = [&](int s) { return bars + 8 * (2 * (KK + KV) + 2 + s); };
+  const uint32_t pv_done = bars + 8 * (2 * (KK + KV) + 4), q_ready = pv_done + 8, rows_bar = pv_done + 16;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   clear_dead_rows<bf16>(a, D);
   Walk<PAGED> w(a, kTcRows);
   if (!w.begin()) return;                                          // (the same answer in every warp)
   if (tid == 0) {
-    for (int s = 0; s < KS; ++s) { tc::mbar_init(k_full(s), 1); tc::mbar_init(k_empty(s), 1); tc::mbar_init(v_full(s), 1); tc::mbar_init(v_empty(s), 1); }
+    for (int s = 0; s < KK; ++s) { tc::mbar_init(k_full(s), 1); tc::mbar_init(k_empty(s), 1); }
+    for (int s = 0; s < KV; ++s) { tc::mbar_init(v_full(s), 1); tc::mbar_init(v_empty(s), 1); }
     for (int s = 0; s < 2; ++s) { tc::mbar_init(s_full(s), 1); tc::mbar_init(p_ready(s), 4); }
     tc::mbar_init(pv_done, 1);
     tc::mbar_init(q_ready, 4);
@@ -127,57 +131,66 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
   volatile int* dead = &s_dead;
 
   if (warp == 4) {
-    // ---- loads: a lane each looks up the pages of 32 chunks, the first lane issues
-    int n = 0;
-    bool ok = true;
-    do {
-      const int cached = w.cache_chunks();
-      int pages = -1;
-      for (int c = w.c_begin; c < w.c_end && ok; ++c, ++n) {
-        const int ahead = (c - w.c_begin) % 32;
-        if (ahead == 0) pages = c + lane < w.c_end ? w.page_of(c + lane) : -1;
-        const int page = __shfl_sync(0xffffffffu, pages, ahead);
-        const int st = n % KS, ph = (n / KS) & 1;
-        if (lane == 0) {
-          const bool node = c >= cached;
-          // (a page that is not there: some page comes instead, all of it masked)
-          const int y = node ? w.b * a.T + (c - cached) * kChunk : max(page, 0) * kPagePos;
-          if ((ok = wait_bar(k_empty(st), ph ^ 1, dead))) {
-            tc::mbar_expect_tx(k_full(st), S::KV_BYTES);
+    // ---- loads: keys and values go their ways independently, each as far ahead as its stages allow
+    if (lane == 0) {
+      Walk<PAGED> wv = w;
+      int nk = 0, nv = 0, ck = w.c_begin, cv = wv.c_begin;
+      int page_k = w.page_of(ck), page_v = page_k;                 // (looked up a chunk ahead)
+      bool k_left = true, v_left = true;
+      auto load = [&](const Walk<PAGED>& at, int c, int page, uint32_t dst, uint32_t bar, const CUtensorMap* pool, const CUtensorMap* drafted) {
+        const int cached = at.cache_chunks();
+        const bool node = c >= cached;
+        // (a page that is not there: some page comes instead, all of it masked)
+        const int y = node ? at.b * a.T + (c - cached) * kChunk : max(page, 0) * kPagePos;
+        tc::mbar_expect_tx(bar, S::KV_BYTES);
 #pragma unroll
-            for (int p = 0; p < S::PANELS; ++p) load_box(k_s + st * S::KV_BYTES + p * S::PANEL, node ? &maps.kn : &maps.kp, k_full(st), w.tl.h * D + p * 64, y);
-            if ((ok = wait_bar(v_empty(st), ph ^ 1, dead))) {
-              s_keys[st] = w.keys_of(c, page);                     // (read until the values before have been used)
-              tc::mbar_expect_tx(v_full(st), S::KV_BYTES);
-#pragma unroll
-              for (int p = 0; p < S::PANELS; ++p) load_box(v_s + st * S::KV_BYTES + p * S::PANEL, node ? &maps.vn : &maps.vp, v_full(st), w.tl.h * D + p * 64, y);
-            } else {
-              tc::mbar_wait(k_full(st), ph);
-            }
-          }
+        for (int p = 0; p < S::PANELS; ++p) load_box(dst + p * S::PANEL, node ? drafted : pool, bar, at.tl.h * D + p * 64, y);
+      };
+      unsigned long long t0 = clock64();
+      while (k_left || v_left) {
+        bool moved = false;
+        if (k_left && tc::mbar_test(k_empty(nk), ((nk / KK) & 1) ^ 1)) {
+          s_keys[nk % 4] = w.keys_of(ck, page_k);                  // (four chunks on, this one's softmax is done)
+          load(w, ck, page_k, k_s + nk % KK * S::KV_BYTES, k_full(nk), &maps.kp, &maps.kn);
+          ++nk;
+          if (++ck >= w.c_end) { k_left = w.next(); ck = w.c_begin; }
+          if (k_left) page_k = w.page_of(ck);
+          moved = true;
         }
-        ok = __shfl_sync(0xffffffffu, ok, 0);
-        if (!ok) break;
+        if (v_left && tc::mbar_test(v_empty(nv), ((nv / KV) & 1) ^ 1)) {
+          load(wv, cv, page_v, v_s + nv % KV * S::KV_BYTES, v_full(nv), &maps.vp, &maps.vn);
+          ++nv;
+          if (++cv >= wv.c_end) { v_left = wv.next(); cv = wv.c_begin; }
+          if (v_left) page_v = wv.page_of(cv);
+          moved = true;
+        }
+        if (moved) {
+          t0 = clock64();
+        } else if (*dead || (unsigned long long)(clock64() - t0) > tc::kSpinCycles) {
+          *dead = 1;
+          break;
+        }
       }
-    } while (ok && w.next());
-    // after an expired wait: copies in flight land before the shared memory goes
-    if (lane == 0 && (!ok || *dead))
-      for (int i = max(0, n - KS); i < n; ++i) { tc::mbar_wait(k_full(i % KS), (i / KS) & 1); tc::mbar_wait(v_full(i % KS), (i / KS) & 1); }
+      // after an expired wait: copies in flight land before the shared memory goes
+      if (*dead) {
+        for (int i = max(0, nk - KK); i < nk; ++i) tc::mbar_wait(k_full(i), (i / KK) & 1);
+        for (int i = max(0, nv - KV); i < nv; ++i) tc::mbar_wait(v_full(i), (i / KV) & 1);
+      }
+    }
   } else if (warp == 5) {
     // ---- products
     if (lane == 0) {
       const uint32_t id_s = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kChunk >> 3) << 17) | ((uint32_t)(kTcRows >> 4) << 24);
       const uint32_t id_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTcRows >> 4) << 24);
       auto scores = [&](int n) {
-        const int st = n % KS;
-        if (!wait_bar(k_full(st), (n / KS) & 1, dead)) return false;
+        if (!wait_bar(k_full(n), (n / KK) & 1, dead)) return false;
         tc::tc_fence_after();
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
           tc::umma_f16(tmem + (n & 1) * 64, tc::smem_desc_sw128(q_s + k / 4 * S::Q_PANEL + (k % 4) * 32),
-                       tc::smem_desc_sw128(k_s + st * S::KV_BYTES + k / 4 * S::PANEL + (k % 4) * 32), id_s, k > 0);
+                       tc::smem_desc_sw128(k_s + n % KK * S::KV_BYTES + k / 4 * S::PANEL + (k % 4) * 32), id_s, k > 0);
         tc::umma_commit(s_full(n & 1));
-        tc::umma_commit(k_empty(st));
+        tc::umma_commit(k_empty(n));
         return true;
       };
       int n = 0, tile = 0;
@@ -188,18 +201,17 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
         const int count = w.c_end - w.c_begin;
         if (ok) ok = scores(n);
         for (int i = 0; i < count && ok; ++i, ++n) {
-          const int st = n % KS;
           // (the next chunk's scores take the place of weights whose product was issued before them)
           if (i + 1 < count && !(ok = scores(n + 1))) break;
-          if (!(ok = wait_bar(p_ready(n & 1), (n >> 1) & 1, dead)) || !(ok = wait_bar(v_full(st), (n / KS) & 1, dead))) break;
+          if (!(ok = wait_bar(p_ready(n & 1), (n >> 1) & 1, dead)) || !(ok = wait_bar(v_full(n), (n / KV) & 1, dead))) break;
           tc::tc_fence_after();
 #pragma unroll
           for (int plane = 0; plane < 2; ++plane)
 #pragma unroll
             for (int k = 0; k < kChunk / 16; ++k)
-              umma_f16_ts(o_tmem, tmem + (n & 1) * 64 + plane * 32 + k * 8, value_desc(v_s + st * S::KV_BYTES + k * 2048, S::PANEL), id_o,
+              umma_f16_ts(o_tmem, tmem + (n & 1) * 64 + plane * 32 + k * 8, value_desc(v_s + n % KV * S::KV_BYTES + k * 2048, S::PANEL), id_o,
                           i > 0 || plane > 0 || k > 0);
-          tc::umma_commit(v_empty(st));
+          tc::umma_commit(v_empty(n));
           tc::umma_commit(pv_done);
         }
         ++tile;
@@ -225,13 +237,24 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
     do {
       const int rows = w.rows(), r = tid, cached = w.cache_chunks(), count = w.c_end - w.c_begin, b = w.b;
       const bool active = warp * 32 < rows;
-      // queries into swizzled shared memory; the outputs of the tile before have been read
-      for (int i = tid; i < ((rows + 31) & ~31) * (D / 8); i += 128) {
-        const int row = i / (D / 8), piece = i % (D / 8);
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (row < rows)
-          x = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(a.q) + ((long long)b * a.T + w.node_of(row)) * a.q_stride + w.head_of(row) * D + piece * 8);
-        *reinterpret_cast<uint4*>(gen + piece / 8 * S::Q_PANEL + row * 128 + ((piece % 8) ^ (row & 7)) * 16) = x;
+      // The warp's queries into swizzled shared memory (its outputs of the tile before have been read), all loads side by side:
+      // 16 trips to L2 one after the other would cost as much as five chunks.
+      if (active) {
+        constexpr int PIECES = D / 8, STEP = 32 / PIECES;          // rows a step
+        uint4 x[PIECES];
+        const int piece = lane % PIECES;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+          const int row = warp * 32 + i * STEP + lane / PIECES;
+          x[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (row < rows)
+            x[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(a.q) + ((long long)b * a.T + w.node_of(row)) * a.q_stride + w.head_of(row) * D + piece * 8);
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+          const int row = warp * 32 + i * STEP + lane / PIECES;
+          *reinterpret_cast<uint4*>(gen + piece / 8 * S::Q_PANEL + row * 128 + ((piece % 8) ^ (row & 7)) * 16) = x[i];
+        }
       }
       fence_async_shared();
       tc::tc_fence_before();
@@ -249,16 +272,16 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
       }
       float m = -INFINITY, l = 0.f;                                // m: what the weights are scaled by, a maximum of the past
       for (int i = 0; i < count; ++i, ++n) {
-        const int c = w.c_begin + i, st = n % KS, sb = n & 1;
+        const int c = w.c_begin + i, sb = n & 1;
         const bool node = c >= cached;
         if (!(ok = wait_bar_warp(s_full(sb), (n >> 1) & 1, dead))) break;
         tc::tc_fence_after();
-        if (!(ok = wait_bar_warp(v_full(st), (n / KS) & 1, dead))) break;
-        const int n_keys = s_keys[st];
+        const int n_keys = s_keys[n % 4];
         const bool partial = n_keys < kChunk || node;
         // keys behind the last: their values become 0; in the tree's chunk so do values that are no finite numbers, see below
         if (partial) {
-          uint8_t* vb = gen + (v_s - base) + st * S::KV_BYTES;
+          if (!(ok = wait_bar_warp(v_full(n), (n / KV) & 1, dead))) break;
+          uint8_t* vb = gen + (v_s - base) + n % KV * S::KV_BYTES;
           for (int j = tid; j < kChunk * (D / 8); j += 128) {
             const int key = j / (D / 8), piece = j % (D / 8);
             uint4* at = reinterpret_cast<uint4*>(vb + piece / 8 * S::PANEL + key * 128 + ((piece % 8) ^ (key & 7)) * 16);
@@ -380,9 +403,20 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
                 }
                 *reinterpret_cast<uint4*>(o + e) = make_uint4(y[0], y[1], y[2], y[3]);
               }
-            } else {
+            }
+          }
+          if (!whole) {
+            // 32 rows x 32 columns through the warp's own rows of the queries' place, so that stores are whole lines
+            uint8_t* mine = gen + warp * 4096;
+            __syncwarp();
 #pragma unroll
-              for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(part + (long long)r * D + d + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+            for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(mine + lane * 128 + (((e / 4) ^ (lane & 7)) * 16)) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+            __syncwarp();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int row = e * 4 + lane / 8, piece = lane % 8;
+              const uint4 y = *reinterpret_cast<const uint4*>(mine + row * 128 + ((piece ^ (row & 7)) * 16));
+              if (warp * 32 + row < rows) *reinterpret_cast<uint4*>(part + (long long)(warp * 32 + row) * D + d + piece * 4) = y;
             }
           }
         }
