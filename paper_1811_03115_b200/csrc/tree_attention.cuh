@@ -115,14 +115,58 @@ struct Shape {
   static constexpr int CTAS_PER_SM = F32 ? (D >= 128 ? 1 : 2) : (D >= 128 ? 2 : 3);
 };
 
-// Bits of the ancestors-or-self of node t among nodes 64 * word .. 64 * word + 63.
-__device__ __forceinline__ unsigned long long line_bits(const int* parents, int t, int word) {
-  unsigned long long bits = 0;
-  while (t >= 0) {
-    if ((t >> 6) == word) bits |= 1ull << (t & 63);
-    t = parent_of(parents[t], t);
+// The nodes' lines as bits: bits[word][t] has those of node t's line among nodes 64 * word ..  By doubling: a node takes over
+// what its current forefather has seen and that one's forefather, so a chain of 128 takes 7 rounds (walked up row by row it took
+// 9 us).  One warp's work: with four, the barriers of the rounds took 7 us.
+struct Lines {
+  unsigned long long bits[kMaxNodes / 64][kMaxNodes];
+  int up[kMaxNodes];
+};
+template <int PER>
+__device__ __forceinline__ void lines_by_warp(Lines& x, const int* parents, int nodes, int lane) {
+  constexpr int W = (PER * 32 + 63) / 64;
+  unsigned long long mine[PER][W];
+  int up[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int t = lane + k * 32;
+    up[k] = t < nodes ? parent_of(parents[t], t) : -1;
+#pragma unroll
+    for (int w = 0; w < W; ++w) mine[k][w] = t / 64 == w ? 1ull << (t % 64) : 0ull;
   }
-  return bits;
+  for (int reach = 1; reach < nodes; reach *= 2) {
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int t = lane + k * 32;
+      x.up[t] = up[k];
+#pragma unroll
+      for (int w = 0; w < W; ++w) x.bits[w][t] = mine[k][w];
+    }
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      if (up[k] < 0) continue;
+#pragma unroll
+      for (int w = 0; w < W; ++w) mine[k][w] |= x.bits[w][up[k]];
+      up[k] = x.up[up[k]];
+    }
+    const bool done = __all_sync(0xffffffffu, [&] { bool d = true;
+#pragma unroll
+      for (int k = 0; k < PER; ++k) d = d && up[k] < 0;
+      return d; }());
+    if (done) break;
+  }
+  __syncwarp();
+#pragma unroll
+  for (int k = 0; k < PER; ++k)
+#pragma unroll
+    for (int w = 0; w < W; ++w) x.bits[w][lane + k * 32] = mine[k][w];
+}
+__device__ __forceinline__ void find_lines(Lines& x, const int* parents, int nodes, int lane) {
+  if (nodes <= 32) lines_by_warp<1>(x, parents, nodes, lane);
+  else if (nodes <= 64) lines_by_warp<2>(x, parents, nodes, lane);
+  else if (nodes <= 128) lines_by_warp<4>(x, parents, nodes, lane);
+  else lines_by_warp<kMaxNodes / 32>(x, parents, nodes, lane);
 }
 
 // Floats of a partial result: outputs [rows][D], maxima, sums; whole 16 bytes, as the outputs go there four at a time.
@@ -266,7 +310,6 @@ struct Walk {
   __device__ __forceinline__ int node_of(int r) const { return PAGED ? tl.t : (tl.r0 + r) / a.G; }
   __device__ __forceinline__ int head_of(int r) const { return tl.h * a.G + (PAGED ? tl.r0 + r : (tl.r0 + r) % a.G); }
   __device__ __forceinline__ long long out_row(int r) const { return ((long long)b * a.T + node_of(r)) * a.H + head_of(r); }
-  __device__ __forceinline__ int tree_chunks() const { return ceil_div(sq.nodes, kChunk); }
   __device__ __forceinline__ int cache_chunks() const { return sq.w.chunks - ceil_div(sq.nodes, kChunk); }
   __device__ __forceinline__ bool whole() const { return c_begin == 0 && c_end == sq.w.chunks; }
   // Page of cache chunk c (-1: none, or a chunk of the tree), and the number of keys in a chunk.
@@ -316,8 +359,8 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
   constexpr int R = S::R, WK = S::WK, KW = S::KW, KT = D / 16, NT = KW / 8, DT = D / 8;
   extern __shared__ __align__(128) uint8_t ta_smem[];
   __shared__ __align__(8) unsigned long long s_full[S::STAGES];
-  __shared__ int s_dead, s_keys[S::STAGES], s_pages[kPagesAhead], s_parents[kMaxNodes];
-  __shared__ unsigned long long s_line[R][kMaxNodes / 64];
+  __shared__ int s_dead, s_keys[S::STAGES], s_pages[kPagesAhead];
+  __shared__ Lines s_lines;
   __shared__ float s_m[WK][R], s_l[WK][R];
   uint8_t* ring = ta_smem + ((1024u - (s_addr(ta_smem) & 1023u)) & 1023u);
   bf16* qs = reinterpret_cast<bf16*>(ring + (S::SMEM - 1024 - S::Q_BYTES));
@@ -328,7 +371,7 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
   clear_dead_rows<CT>(a, D);
   Walk<PAGED> w(a, R);
   if (!w.begin()) return;
-  int lines_of = -1;                                        // sequence whose parents are in shared memory
+  int lines_of = -1;                                        // sequence whose lines are in shared memory
   int n = 0;                                                // chunks so far
   if (TMA) {
     if (tid == 0) {
@@ -345,7 +388,6 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
     auto head_of = [&](int r) { return w.head_of(r); };
     const Tile& tl = w.tl;
     const Seq& sq = w.sq;
-    const int tree_chunks = w.tree_chunks();
     // Pages of the chunks from c0 on, and a barrier.
     auto look_up = [&](int c0) {
       for (int i = tid; i < kPagesAhead && c0 + i < c_end; i += kThreads) s_pages[i] = w.page_of(c0 + i);
@@ -423,16 +465,10 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
       }
     }
     // the rows' lines in the tree, where the run reaches it
-    if (c_end > cache_chunks) {
-      if (lines_of != b) {
-        for (int i = tid; i < sq.nodes; i += kThreads) s_parents[i] = a.parents[(long long)b * a.T + i];
-        lines_of = b;
-      }
-      __syncthreads();
-      for (int i = tid; i < R * tree_chunks; i += kThreads) {
-        const int r = i % R, w = i / R;
-        s_line[r][w] = r < rows ? line_bits(s_parents, node_of(r), w) : 0ull;
-      }
+    if (c_end > cache_chunks && lines_of != b) {
+      __syncthreads();                                      // (those of the sequence before have been used)
+      if (warp == 0) find_lines(s_lines, a.parents + (long long)b * a.T, sq.nodes, lane);   // (a barrier follows: look_up's)
+      lines_of = b;
     }
 
     float o[DT][4];
@@ -518,7 +554,9 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
 
       // what the rows do not see
       if (c >= cache_chunks) {
-        const unsigned long long line0 = s_line[wr * 16 + g][c - cache_chunks], line1 = s_line[wr * 16 + g + 8][c - cache_chunks];
+        const int r0 = wr * 16 + g;
+        const unsigned long long line0 = r0 < rows ? s_lines.bits[c - cache_chunks][node_of(r0)] : 0ull;
+        const unsigned long long line1 = r0 + 8 < rows ? s_lines.bits[c - cache_chunks][node_of(r0 + 8)] : 0ull;
 #pragma unroll
         for (int i = 0; i < NT; ++i)
 #pragma unroll

@@ -61,6 +61,11 @@ __device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) 
       "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::BPD_TMEM_32(BPD_IN, r), "r"(at) : "memory");
 #undef BPD_IN
 }
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+               "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(at) : "memory");
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -99,7 +104,8 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
   const uint32_t q_s = base, k_s = q_s + S::Q_BYTES, v_s = k_s + KK * S::KV_BYTES;
   __shared__ __align__(8) unsigned long long s_bar[2 * (KK + KV) + 7];
   __shared__ uint32_t s_tmem;
-  __shared__ int s_dead, s_odd, s_keys[4], s_parents[kMaxNodes];
+  __shared__ int s_dead, s_odd, s_keys[4];
+  __shared__ Lines s_lines;
   const uint32_t bars = s_addr(s_bar);
   auto k_full = [&](int n) { return bars + 8 * (n % KK); };         // of chunk n (of the CTA's)
   auto k_empty = [&](int n) { return bars + 8 * (KK + n % KK); };
@@ -121,6 +127,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
     tc::mbar_init(q_ready, 4);
     tc::mbar_init(rows_bar, 4);
     s_dead = 0;
+    s_odd = 0;                                                     // the last tile that had such values
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 5) tc::tmem_alloc(s_addr(&s_tmem), S::TMEM_COLS);
@@ -226,9 +233,9 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
   } else {
     // ---- softmax: a thread per row
     const uint32_t my = (uint32_t)(warp * 32) << 16;
-    int n = 0, lines_of = -1, met = 0;
+    int n = 0, tile = 0, lines_of = -1, met = 0;
     bool ok = true;
-    // the four warps meet
+    // the four warps meet (what one of them wrote to shared memory, the others see)
     auto meet = [&] {
       __syncwarp();
       if (lane == 0) mbar_arrive(rows_bar);
@@ -261,13 +268,11 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
       __syncwarp();
       if (lane == 0) mbar_arrive(q_ready);
       const bool tree = w.c_end > cached;
-      if (tree) {
-        if (!(ok = meet())) break;
-        if (lines_of != b) {
-          for (int i = tid; i < w.sq.nodes; i += 128) s_parents[i] = a.parents[(long long)b * a.T + i];
-          lines_of = b;
-        }
-        if (tid == 0) s_odd = 0;
+      ++tile;
+      if (tree && lines_of != b) {
+        if (!(ok = meet())) break;                                 // (those of the sequence before have been used)
+        if (warp == 0) find_lines(s_lines, a.parents + (long long)b * a.T, w.sq.nodes, lane);
+        lines_of = b;
         if (!(ok = meet())) break;
       }
       float m = -INFINITY, l = 0.f;                                // m: what the weights are scaled by, a maximum of the past
@@ -296,7 +301,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
                 if ((x[e] & 0x7f80u) == 0x7f80u) { x[e] &= 0xffff0000u; odd = true; }
                 if ((x[e] & 0x7f800000u) == 0x7f800000u) { x[e] &= 0x0000ffffu; odd = true; }
               }
-              if (odd) { *at = v; s_odd = 1; }
+              if (odd) { *at = v; s_odd = tile; }
             }
           }
           fence_async_shared();
@@ -312,7 +317,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
           }
           if (partial) {
             unsigned long long see = n_keys >= 64 ? ~0ull : (1ull << n_keys) - 1;
-            if (node) see &= r < rows ? line_bits(s_parents, w.node_of(r), c - cached) : 0ull;
+            if (node) see &= r < rows ? s_lines.bits[c - cached][w.node_of(r)] : 0ull;
 #pragma unroll
             for (int j = 0; j < 64; ++j) if (!((see >> j) & 1)) s[j] = 0xff800000u;
           }
@@ -342,20 +347,24 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
           }
           const float ref = m == -INFINITY ? 0.f : m;
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
-          uint32_t hi[32], lo[32];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const float p0 = exp2_fast(fmaf(__uint_as_float(s[2 * j]), a.scale_log2, -ref)), p1 = exp2_fast(fmaf(__uint_as_float(s[2 * j + 1]), a.scale_log2, -ref));
-            sum[j & 3] += p0 + p1;
-            // the high plane is the weight cut off behind 8 bits, the low plane what is left, rounded
-            hi[j] = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
-            const __nv_bfloat162 rest = __floats2bfloat162_rn(p0 - __uint_as_float(__float_as_uint(p0) & 0xffff0000u),
-                                                              p1 - __uint_as_float(__float_as_uint(p1) & 0xffff0000u));
-            lo[j] = *reinterpret_cast<const uint32_t*>(&rest);
+          for (int half = 0; half < 2; ++half) {
+            uint32_t hi[16], lo[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const int at = half * 32 + 2 * j;
+              const float p0 = exp2_fast(fmaf(__uint_as_float(s[at]), a.scale_log2, -ref)), p1 = exp2_fast(fmaf(__uint_as_float(s[at + 1]), a.scale_log2, -ref));
+              sum[j & 3] += p0 + p1;
+              // the high plane is the weight cut off behind 8 bits, the low plane what is left, rounded
+              hi[j] = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
+              const __nv_bfloat162 rest = __floats2bfloat162_rn(p0 - __uint_as_float(__float_as_uint(p0) & 0xffff0000u),
+                                                                p1 - __uint_as_float(__float_as_uint(p1) & 0xffff0000u));
+              lo[j] = *reinterpret_cast<const uint32_t*>(&rest);
+            }
+            tmem_st16(tmem + my + sb * 64 + half * 16, hi);
+            tmem_st16(tmem + my + sb * 64 + 32 + half * 16, lo);
           }
           l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-          tmem_st32(tmem + my + sb * 64, hi);
-          tmem_st32(tmem + my + sb * 64 + 32, lo);
           tmem_wait_st();
         }
         tc::tc_fence_before();
@@ -367,7 +376,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
       if (!(ok = wait_bar_warp(pv_done, (n - 1) & 1, dead))) break;
       tc::tc_fence_after();
       if (tree && !(ok = meet())) break;
-      const bool whole = w.whole(), odd = tree && s_odd;
+      const bool whole = w.whole(), odd = tree && s_odd == tile;
       if (active) {
         const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
         const long long at = r < rows ? w.out_row(r) : 0;
@@ -380,9 +389,9 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
           if (r < rows) {
             // Values that were no finite numbers: a row that sees one has no finite output there, whatever its weight.
             if (odd) {
-              const int node0 = max(0, w.c_begin - cached) * kChunk, node1 = (w.c_end - cached) * kChunk;
-              for (int t = w.node_of(r); t >= 0; t = parent_of(s_parents[t], t)) {
-                if (t < node0 || t >= node1) continue;
+              const int node1 = min(w.sq.nodes, (w.c_end - cached) * kChunk);
+              for (int t = max(0, w.c_begin - cached) * kChunk; t < node1; ++t) {
+                if (!((s_lines.bits[t / 64][w.node_of(r)] >> (t % 64)) & 1)) continue;
                 const bf16* v = reinterpret_cast<const bf16*>(a.v_new) + ((long long)b * a.T + t) * a.kv_stride + w.tl.h * D + d;
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
