@@ -105,6 +105,26 @@ int check_scratch(const void* scratch, size_t have, size_t need) {
 }
 
 template <typename CT>
+int launch_select(SelectArgs& a, int D, cudaStream_t st) {
+  const long long items = (long long)a.B * a.T * a.Hkv;
+  // CTAs for every SM; a share of at least 64 pages each
+  a.cluster = 1;
+  while (a.cluster < 8 && items * a.cluster * 2 <= kSMs && a.ppr >= a.cluster * 128) a.cluster *= 2;
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3((unsigned)(items * a.cluster)); cfg.blockDim = dim3(kSelectThreads); cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)a.cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = a.cluster > 1 ? 1 : 0;
+  void* ptrs[] = {&a};
+  BPD_TREE_BY_DIM(BPD_CUDA(cudaLaunchKernelExC(&cfg, reinterpret_cast<const void*>(page_select_kernel<CT, DD>), ptrs)); break;)
+  ++g_launches;
+  return BPD_OK;
+}
+
+template <typename CT>
 int launch_weights(const WeightArgs& a, int D, cudaStream_t st) {
   const dim3 grid(a.B * a.Hkv, ceil_div(a.ppr, kWPages));
   BPD_TREE_BY_DIM(BPD_CUDA(launch_k(cache_weights_kernel<CT, DD>, grid, dim3(kWThreads), 0, st, false, a)); break;)
@@ -181,14 +201,11 @@ int bpd_op_page_attention(const bpd_cache* cache, const float* means, const void
   char* base = static_cast<char*>(scratch);
   SelectArgs p;
   p.q = q; p.means = means; p.lens = lens; p.nodes = n_nodes; p.B = shape.B; p.T = nodes; p.H = heads; p.Hkv = shape.Hkv; p.G = shape.G;
-  p.D = cache->head_dim; p.ppr = shape.ppr; p.select = select; p.q_stride = q_stride;
+  p.ppr = shape.ppr; p.select = select; p.q_stride = q_stride;
   p.keys = reinterpret_cast<unsigned long long*>(base + plan.part_bytes + plan.info_bytes);
   p.pages = pages ? pages : reinterpret_cast<int*>(base + plan.part_bytes + plan.info_bytes + s.keys);
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  const dim3 grid(shape.B * nodes * shape.Hkv);
-  if (cache->dtype == 0) BPD_CUDA(launch_k(page_select_kernel<float>, grid, dim3(kSelectThreads), 0, st, false, p));
-  else BPD_CUDA(launch_k(page_select_kernel<bf16>, grid, dim3(kSelectThreads), 0, st, false, p));
-  ++g_launches;
+  if ((rc = cache->dtype == 0 ? launch_select<float>(p, cache->head_dim, st) : launch_select<bf16>(p, cache->head_dim, st))) return rc;
   return attend(cache, q, k_new, v_new, nodes, heads, q_stride, kv_stride, lens, parents, n_nodes, scale, true, select, p.pages, plan, base,
                 out, lse, st);
 }

@@ -377,35 +377,63 @@ struct MeansArgs {
 };
 
 // Means of the keys of the pages that have become full.  Sums are in 64 bits and rounded once: selections go by them, and
-// a sum whose rounding depends on its order would make near ties depend on it too.  grid (ppr, B, layers), a thread per four
-// columns.
-constexpr int kMeansThreads = 128;
+// a sum whose rounding depends on its order would make near ties depend on it too.  grid (ppr, B, layers): a CTA per page, a
+// thread per 16 bytes of columns and group of positions, eight loads under way at once.  Bound by reading the keys where many
+// pages are new (several CTAs share an SM then, and one's sums run under the others' loads; with 512 threads and 16 loads each,
+// one CTA to an SM, 8 sequences of up to 60000 took 250 us instead of 110), by a few trips to memory where few are.
+constexpr int kMeansThreads = 256, kMeansBatch = 8;
 template <typename CT>
-__global__ void __launch_bounds__(kMeansThreads) page_means_kernel(const __grid_constant__ MeansArgs a) {
+__global__ void __launch_bounds__(kMeansThreads, 3) page_means_kernel(const __grid_constant__ MeansArgs a) {
+  constexpr int PER = 16 / (int)sizeof(CT);
+  __shared__ double s_sum[PER][kMeansThreads];
   const int p = blockIdx.x, b = blockIdx.y, layer = blockIdx.z, cap = a.ppr * kPagePos;
   if (p >= clamp_int(a.lens[b], 0, cap) / kPagePos || p < clamp_int(a.from[b], 0, cap) / kPagePos) return;
-  const int page = a.table[(long long)b * a.ppr + p];
-  const long long row = pool_row(page, a.n_pages, 0);
+  const long long row = pool_row(a.table[(long long)b * a.ppr + p], a.n_pages, 0);
   if (row < 0) return;
   const CT* src = reinterpret_cast<const CT*>(a.k_pool) + ((long long)layer * a.n_pages * kPagePos + row) * a.width;
   float* out = a.means + (((long long)layer * a.B + b) * a.ppr + p) * a.width;
-  for (int c = threadIdx.x * 4; c < a.width; c += kMeansThreads * 4) {
-    double s[4] = {0., 0., 0., 0.};
-#pragma unroll 8
-    for (int r = 0; r < kPagePos; ++r) {
-      float v[4];
-      if constexpr (sizeof(CT) == 4) {
-        const float4 x = *reinterpret_cast<const float4*>(src + (long long)r * a.width + c);
-        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-      } else {
-        const uint2 x = *reinterpret_cast<const uint2*>(src + (long long)r * a.width + c);
-        v[0] = __uint_as_float(x.x << 16); v[1] = __uint_as_float(x.x & 0xffff0000u);
-        v[2] = __uint_as_float(x.y << 16); v[3] = __uint_as_float(x.y & 0xffff0000u);
-      }
+  const int pieces = a.width / PER;
+  // groups of positions: as many as there are threads for (a power of two, so that they divide the page), of a batch at least
+  int groups = 1;
+  while (groups < kPagePos / kMeansBatch && pieces * groups * 2 <= kMeansThreads) groups *= 2;
+  const int across = kMeansThreads / groups, g = threadIdx.x / across, rows = kPagePos / groups;
+  for (int c0 = 0; c0 < pieces; c0 += across) {
+    const int c = c0 + threadIdx.x % across;
+    double s[PER];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] += (double)v[e];
+    for (int e = 0; e < PER; ++e) s[e] = 0.;
+    if (c < pieces) {
+      const CT* at = src + (long long)g * rows * a.width + c * PER;
+      for (int r0 = 0; r0 < rows; r0 += kMeansBatch) {
+        uint4 v[kMeansBatch];
+#pragma unroll
+        for (int r = 0; r < kMeansBatch; ++r) v[r] = *reinterpret_cast<const uint4*>(at + (long long)(r0 + r) * a.width);
+#pragma unroll
+        for (int r = 0; r < kMeansBatch; ++r) {
+          const uint32_t x[4] = {v[r].x, v[r].y, v[r].z, v[r].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(CT) == 4) {
+              s[e] += (double)__uint_as_float(x[e]);
+            } else {
+              s[2 * e] += (double)__uint_as_float(x[e] << 16);
+              s[2 * e + 1] += (double)__uint_as_float(x[e] & 0xffff0000u);
+            }
+          }
+        }
+      }
     }
-    *reinterpret_cast<float4*>(out + c) = make_float4((float)(s[0] / kPagePos), (float)(s[1] / kPagePos), (float)(s[2] / kPagePos), (float)(s[3] / kPagePos));
+#pragma unroll
+    for (int e = 0; e < PER; ++e) s_sum[e][threadIdx.x] = s[e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < across * PER; i += kMeansThreads) {
+      const int col = i % across, e = i / across;
+      if (c0 + col >= pieces) continue;
+      double sum = 0.;
+      for (int k = 0; k < groups; ++k) sum += s_sum[e][k * across + col];
+      out[(c0 + col) * PER + e] = (float)(sum / kPagePos);
+    }
+    __syncthreads();
   }
 }
 
@@ -414,103 +442,156 @@ struct SelectArgs {
   const void* q;
   const float* means;                  // [B][ppr][Hkv][D]
   const int *lens, *nodes;
-  int B, T, H, Hkv, G, D, ppr, select;
+  int B, T, H, Hkv, G, ppr, select, cluster;
   long long q_stride;
   unsigned long long* keys;            // scratch [B][T][Hkv][ppr]
   int* pages;                          // [B][T][Hkv][select]
 };
 
 // score(page) = (sum of the group's queries) . mean, in 64 bits: the border of a selection is often close.  The best
-// `select` full pages (ties and NaN: the lower page, NaN below everything), listed in ascending order.  A CTA per (node,
-// key head).
-constexpr int kSelectThreads = 256;
-template <typename CT>
+// `select` full pages (ties and NaN: the lower page, NaN below everything), listed in ascending order.
+//
+// A cluster per (node, key head): its CTAs score a share of the pages each -- a warp takes eight pages at a time and adds up
+// their eight sums together -- and the first one finds the border bit by bit, from the top: a candidate stands if at least
+// `select` keys are not below it, and ends the search where it is exactly so many.  A candidate costs one barrier that counts
+// (the scores of a sequence differ in their first bits, so some 20 candidates do); histograms of digits, with their atomics
+// and scans, took five times as long.
+constexpr int kSelectThreads = 256, kSelectKept = 8;    // keys a thread keeps in registers
+template <typename CT, int D>
 __global__ void __launch_bounds__(kSelectThreads) page_select_kernel(const __grid_constant__ SelectArgs a) {
-  __shared__ double s_q[128];
-  __shared__ int s_hist[256], s_warp[kSelectThreads / 32], s_pick[2];
-  const int id = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  constexpr int WARPS = kSelectThreads / 32, E = D >= 32 ? D / 32 : 1, BATCH = 8;
+  __shared__ double s_q[D];
+  __shared__ int s_warp[WARPS];
+  pdl_launch_dependents();
+  const int id = blockIdx.x / a.cluster, rank = blockIdx.x % a.cluster, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int h = id % a.Hkv, t = id / a.Hkv % a.T, b = id / a.Hkv / a.T;
   int* out = a.pages + (long long)id * a.select;
   const int full = clamp_int(a.lens[b], 0, a.ppr * kPagePos) / kPagePos;
   const bool alive = !a.nodes || t < a.nodes[b];
   const int n_out = alive ? min(full, a.select) : 0;
-  for (int i = n_out + tid; i < a.select; i += kSelectThreads) out[i] = -1;
+  // (these returns are the whole cluster's)
+  if (rank == 0) for (int i = n_out + tid; i < a.select; i += kSelectThreads) out[i] = -1;
   if (n_out == 0) return;
   if (full <= a.select) {
-    for (int i = tid; i < full; i += kSelectThreads) out[i] = i;
+    if (rank == 0) for (int i = tid; i < full; i += kSelectThreads) out[i] = i;
     return;
   }
-  for (int d = tid; d < a.D; d += kSelectThreads) {
+  if (tid < D) {
     double s = 0.;
-    const CT* src = reinterpret_cast<const CT*>(a.q) + ((long long)b * a.T + t) * a.q_stride + h * a.G * a.D + d;
-    for (int g = 0; g < a.G; ++g) s += (double)to_f(src[g * a.D]);
-    s_q[d] = s;
+    const CT* src = reinterpret_cast<const CT*>(a.q) + ((long long)b * a.T + t) * a.q_stride + h * a.G * D + tid;
+    for (int g = 0; g < a.G; ++g) s += (double)to_f(src[g * D]);
+    s_q[tid] = s;
   }
   __syncthreads();
   unsigned long long* keys = a.keys + (long long)id * a.ppr;
-  for (int p = warp; p < full; p += kSelectThreads / 32) {
-    const float* m = a.means + (((long long)b * a.ppr + p) * a.Hkv + h) * a.D;
-    double s = 0.;
-    for (int d = lane; d < a.D; d += 32) s += s_q[d] * (double)m[d];
+  {
+    double q[E];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (lane == 0) keys[p] = s != s ? 0ull : order_bits64(s + 0.);
-  }
-  __threadfence_block();
-  __syncthreads();
-  unsigned long long prefix = 0, mask = 0;
-  int need = a.select;
-  for (int shift = 56; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += kSelectThreads) s_hist[i] = 0;
-    __syncthreads();
-    for (int p = tid; p < full; p += kSelectThreads) {
-      const unsigned long long k = keys[p];
-      if ((k & mask) == prefix) atomicAdd(&s_hist[(k >> shift) & 255], 1);
-    }
-    __syncthreads();
-    if (warp == 0) {
-      int above = 0;
-      for (int top = 224; top >= 0; top -= 32) {
-        const int n = s_hist[top + 31 - lane];
-        int upto = n;
+    for (int e = 0; e < E; ++e) q[e] = lane * E + e < D ? s_q[lane * E + e] : 0.;
+    const float* m = a.means + ((long long)b * a.ppr * a.Hkv + h) * D + (lane * E < D ? lane * E : 0);
+    const long long step = (long long)a.Hkv * D;
+    for (int p0 = (rank * WARPS + warp) * BATCH; p0 < full; p0 += a.cluster * WARPS * BATCH) {
+      float x[BATCH][E];
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += x; }
-        const unsigned hit = __ballot_sync(0xffffffffu, above + upto >= need);
-        if (hit) {
-          const int at = __ffs(hit) - 1;
-          if (lane == at) { s_pick[0] = top + 31 - lane; s_pick[1] = need - (above + upto - n); }
-          break;
-        }
-        above += __shfl_sync(0xffffffffu, upto, 31);
+      for (int k = 0; k < BATCH; ++k) {
+        const float* src = m + min(p0 + k, full - 1) * step;
+        if constexpr (E == 4) *reinterpret_cast<float4*>(x[k]) = *reinterpret_cast<const float4*>(src);
+        else if constexpr (E == 2) *reinterpret_cast<float2*>(x[k]) = *reinterpret_cast<const float2*>(src);
+        else x[k][0] = *src;
       }
+      double s[BATCH];
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        s[k] = 0.;
+#pragma unroll
+        for (int e = 0; e < E; ++e) if (lane * E < D) s[k] += q[e] * (double)x[k][e];
+      }
+      // eight sums over 32 lanes: each step halves the sums a lane carries on with
+#pragma unroll
+      for (int o = 16, k = BATCH / 2; o >= 4; o >>= 1, k >>= 1) {
+#pragma unroll
+        for (int i = 0; i < k; ++i) {
+          const bool up = lane & o;
+          const double give = up ? s[i] : s[i + k], keep = up ? s[i + k] : s[i];
+          s[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+      }
+      s[0] += __shfl_xor_sync(0xffffffffu, s[0], 1);
+      s[0] += __shfl_xor_sync(0xffffffffu, s[0], 2);
+      // the lane's page: bits 4, 3, 2 of its number chose the halves
+      const int p = p0 + ((lane >> 4) & 1) * 4 + ((lane >> 3) & 1) * 2 + ((lane >> 2) & 1);
+      if ((lane & 3) == 0 && p < full) keys[p] = s[0] != s[0] ? 0ull : order_bits64(s[0] + 0.);
     }
-    __syncthreads();
-    prefix |= (unsigned long long)s_pick[0] << shift;
-    mask |= 255ull << shift;
-    need = s_pick[1];
+  }
+  if (a.cluster > 1) {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (rank > 0) return;
+  } else {
+    __threadfence_block();
     __syncthreads();
   }
+  unsigned long long mine[kSelectKept];
+#pragma unroll
+  for (int k = 0; k < kSelectKept; ++k) mine[k] = tid + k * kSelectThreads < full ? __ldcg(keys + tid + k * kSelectThreads) : 0ull;
+  constexpr int KEPT = kSelectKept * kSelectThreads;
+  const int rounds = (full + KEPT - 1) / KEPT;
+  // how many keys are at least x (x > 0: what is behind the last page counts as 0)
+  auto count = [&](unsigned long long x) {
+    int n = 0;
+    for (int r = 0; r < rounds; ++r) {
+      int hits = 0;
+#pragma unroll
+      for (int k = 0; k < kSelectKept; ++k) {
+        const int p = r * KEPT + tid + k * kSelectThreads;
+        const unsigned long long key = r == 0 ? mine[k] : (p < full ? __ldcg(keys + p) : 0ull);
+        hits += key >= x;
+      }
+      n += hits;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+    __syncthreads();
+    if (lane == 0) s_warp[warp] = n;
+    __syncthreads();
+    n = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) n += s_warp[w];
+    return n;
+  };
+  unsigned long long border = 0;
+  bool exact = false;
+  for (int bit = 63; bit >= 0 && !exact; --bit) {
+    const unsigned long long candidate = border | (1ull << bit);
+    const int n = count(candidate);
+    if (n >= a.select) border = candidate;
+    exact = n == a.select;
+  }
+  // keys above the border stay, of those equal to it the lowest pages
+  int room = exact ? full : a.select - (border == ~0ull ? 0 : count(border + 1));
   int ties = 0, done = 0;
   for (int p0 = 0; p0 < full; p0 += kSelectThreads) {
     const int p = p0 + tid;
-    const unsigned long long k = p < full ? keys[p] : 0ull;
-    const bool tie = p < full && k == prefix;
-    bool in = p < full && k > prefix;
+    const unsigned long long k = p < full ? __ldcg(keys + p) : 0ull;
+    const bool tie = p < full && k == border;
+    bool in = p < full && k > border;
     unsigned m = __ballot_sync(0xffffffffu, tie);
+    __syncthreads();
     if (lane == 0) s_warp[warp] = __popc(m);
     __syncthreads();
     int before = ties, all = 0;
-    for (int i = 0; i < kSelectThreads / 32; ++i) { if (i < warp) before += s_warp[i]; all += s_warp[i]; }
-    if (tie && before + __popc(m & ((1u << lane) - 1)) < need) in = true;
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) { if (i < warp) before += s_warp[i]; all += s_warp[i]; }
+    if (tie && before + __popc(m & ((1u << lane) - 1)) < room) in = true;
     ties += all;
     m = __ballot_sync(0xffffffffu, in);
     __syncthreads();
     if (lane == 0) s_warp[warp] = __popc(m);
     __syncthreads();
     int at = done;
-    for (int i = 0; i < kSelectThreads / 32; ++i) { if (i < warp) at += s_warp[i]; done += s_warp[i]; }
-    if (in) out[at + __popc(m & ((1u << lane) - 1))] = p;
-    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) { if (i < warp) at += s_warp[i]; done += s_warp[i]; }
+    at += __popc(m & ((1u << lane) - 1));
+    if (in && at < a.select) out[at] = p;
   }
 }
 

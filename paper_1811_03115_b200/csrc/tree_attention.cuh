@@ -371,6 +371,7 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
   clear_dead_rows<CT>(a, D);
   Walk<PAGED> w(a, R);
   if (!w.begin()) return;
+  if (PAGED) pdl_wait();                                    // the selection
   int lines_of = -1;                                        // sequence whose lines are in shared memory
   int n = 0;                                                // chunks so far
   if (TMA) {

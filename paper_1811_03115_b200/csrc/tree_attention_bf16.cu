@@ -45,7 +45,7 @@ int launch_tc(const AttnArgs& a, const TcMaps& maps, const AttnPlan& p, cudaStre
   using S = TcShape<D>;
   int rc = ensure_smem_limit(reinterpret_cast<const void*>(tree_attention_tc_kernel<D, PAGED>), S::SMEM);
   if (rc) return rc;
-  BPD_CUDA(launch_k(tree_attention_tc_kernel<D, PAGED>, dim3(p.ctas), dim3(kTcThreads), S::SMEM, st, false, a, maps));
+  BPD_CUDA(launch_k(tree_attention_tc_kernel<D, PAGED>, dim3(p.ctas), dim3(kTcThreads), S::SMEM, st, PAGED, a, maps));
   ++g_launches;
   return launch_combine<bf16, D, PAGED>(a, p, st);
 }

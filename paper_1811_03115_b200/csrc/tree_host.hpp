@@ -62,7 +62,7 @@ int launch_one(const AttnArgs& a, const TcMaps& maps, const AttnPlan& p, cudaStr
   const auto kernel = tree_attention_kernel<CT, D, WR, PAGED, TMA>;
   int rc = ensure_smem_limit(reinterpret_cast<const void*>(kernel), S::SMEM);
   if (rc) return rc;
-  BPD_CUDA(launch_k(kernel, dim3(p.ctas), dim3(kThreads), S::SMEM, st, false, a, maps));
+  BPD_CUDA(launch_k(kernel, dim3(p.ctas), dim3(kThreads), S::SMEM, st, PAGED, a, maps));
   ++g_launches;
   return p.split ? launch_combine<CT, D, PAGED>(a, p, st) : BPD_OK;
 }
