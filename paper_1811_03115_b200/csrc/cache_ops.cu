@@ -98,6 +98,9 @@ int check_attention(const bpd_cache* c, const void* q, const void* k_new, const 
       (rc = check_rows(c, v_new, kv_stride, (long long)c->kv_heads * c->head_dim, "v_new"))) return rc;
   return BPD_OK;
 }
+// The most entries of a list that an eviction moves: from above the budget to below it.
+int moves_cap(const bpd_cache* c, int budget) { return std::max(1, std::min(budget, c->pages_per_row * kPagePos - std::min(budget, c->pages_per_row * kPagePos))); }
+
 int check_scratch(const void* scratch, size_t have, size_t need) {
   if (!scratch || !aligned(scratch, 256)) return fail(BPD_E_INVALID, "scratch is null or misaligned");
   if (have < need) return fail(BPD_E_NOMEM, "scratch too small: %zu bytes, %zu needed", have, need);
@@ -254,7 +257,8 @@ int bpd_op_cache_weights(const bpd_cache* cache, const void* q, int nodes, int h
 
 size_t bpd_op_cache_evict_scratch_bytes(const bpd_cache* cache, int budget) {
   if (check_cache(cache, true) || budget < 1) return 0;
-  return round256((size_t)cache->layers * cache->batch * cache->kv_heads * 2 * std::min(budget, cache->pages_per_row * kPagePos) * 4);
+  const size_t lists = (size_t)cache->layers * cache->batch * cache->kv_heads;
+  return round256(lists * moves_cap(cache, budget) * 8) + round256(lists * 4);
 }
 
 int bpd_op_cache_evict(const bpd_cache* cache, const int32_t* lens, const int32_t* seen, int budget, int recent, float* weights,
@@ -271,9 +275,22 @@ int bpd_op_cache_evict(const bpd_cache* cache, const int32_t* lens, const int32_
   a.k_pool = cache->k_pool; a.v_pool = cache->v_pool; a.table = cache->page_table; a.lens = lens; a.seen = seen; a.layers = cache->layers;
   a.B = cache->batch; a.Hkv = cache->kv_heads; a.row_pieces = cache->head_dim * elem_of(cache) / 16; a.ppr = cache->pages_per_row;
   a.n_pages = cache->n_pages; a.budget = budget; a.recent = recent; a.weights = weights; a.positions = positions; a.out_lens = out_lens;
-  a.moves = static_cast<int*>(scratch); a.moves_cap = std::min(budget, a.ppr * kPagePos);
-  BPD_CUDA(launch_k(cache_evict_kernel, dim3(a.layers * a.B * a.Hkv), dim3(kEvictThreads), 0, (cudaStream_t)cuda_stream, false, a));
+  const int lists = a.layers * a.B * a.Hkv;
+  a.moves = static_cast<int2*>(scratch); a.moves_cap = moves_cap(cache, budget);
+  a.counts = reinterpret_cast<int*>(static_cast<char*>(scratch) + round256((size_t)lists * a.moves_cap * 8));
+  // Up to 128 entries a list move within the launch that selects them (a block over the budget: 522 entries of 48 lists, EVICT1);
+  // more are shared by all SMs in a launch of their own (256 lists of up to 8000: EVICT2).
+  a.move_here = a.moves_cap <= 128 ? 1 : 0;
+  if (a.ppr * kPagePos <= 16 * kEvictThreads) BPD_CUDA(launch_k(cache_evict_kernel<16>, dim3(lists), dim3(kEvictThreads), 0, (cudaStream_t)cuda_stream, false, a));
+  else BPD_CUDA(launch_k(cache_evict_kernel<32>, dim3(lists), dim3(kEvictThreads), 0, (cudaStream_t)cuda_stream, false, a));
   ++g_launches;
+  if (!a.move_here) {
+    // parts of at least eight turns of a CTA; more of them where lists are few
+    const long long turns = (long long)a.moves_cap * 2 * a.row_pieces / (kMoveThreads * 8) + 1;
+    const int parts = (int)std::max<long long>(1, std::min<long long>(turns, std::max(2, 8 * kSMs / lists)));
+    BPD_CUDA(launch_k(cache_move_kernel, dim3(lists, parts), dim3(kMoveThreads), 0, (cudaStream_t)cuda_stream, true, a));
+    ++g_launches;
+  }
   return BPD_OK;
 }
 

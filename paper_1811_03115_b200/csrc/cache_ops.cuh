@@ -237,135 +237,221 @@ __global__ void __launch_bounds__(kWThreads) cache_weights_kernel(const __grid_c
 struct EvictArgs {
   void *k_pool, *v_pool;               // [layers][n_pages][64][Hkv][D]
   const int *table, *lens, *seen;
-  int layers, B, Hkv, row_pieces, ppr, n_pages, budget, recent;   // row_pieces: 16-byte pieces of a head's keys
+  int layers, B, Hkv, row_pieces, ppr, n_pages, budget, recent;   // row_pieces: 16-byte pieces of a head's keys, a power of two
   float* weights;                      // [layers][B][Hkv][ppr * 64]
   int* positions;
   int* out_lens;
-  int* moves;                          // scratch: [layers * B * Hkv][2][min(budget, capacity)] slots: holes, and what fills them
+  int2* moves;                         // scratch: [layers * B * Hkv][moves_cap] slots (to, from)
+  int* counts;                         // scratch: [layers * B * Hkv] of them
   int moves_cap;
+  int move_here;                       // 1: the selecting CTA moves the rows itself
 };
 
-// Weight as a number whose unsigned order is the order of eviction: NaN below everything, -0 like 0.
-__device__ __forceinline__ unsigned evict_key(float w) { return w != w ? 0u : order_bits(w + 0.f); }
+// The rows of moves first, first + step, ... of a list.  Sources lie at or above the budget, targets below it: no row is read
+// after it was written, in whatever order they move.  Eight rows' pieces a thread are under way at once.
+__device__ __forceinline__ void move_rows(const EvictArgs& a, int list, int n, long long first, long long step) {
+  const int h = list % a.Hkv, b = list / a.Hkv % a.B, layer = list / a.Hkv / a.B;
+  const int* table = a.table + (long long)b * a.ppr;
+  const int2* moves = a.moves + (long long)list * a.moves_cap;
+  const int shift = 31 - __clz(2 * a.row_pieces);           // pieces of an entry, keys and values
+  const long long layer_rows = (long long)layer * a.n_pages * kPagePos, total = (long long)n << shift;
+  constexpr int AT_ONCE = 8;
+  for (long long i0 = first; i0 < total; i0 += step * AT_ONCE) {
+    uint4 x[AT_ONCE];
+    uint4* to[AT_ONCE];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+      const long long i = i0 + step * k;
+      to[k] = nullptr;
+      if (i >= total) continue;
+      const int2 m = moves[i >> shift];
+      const int rest = (int)(i & ((1 << shift) - 1)), piece = rest & (a.row_pieces - 1);
+      const long long rt = pool_row(table[m.x / kPagePos], a.n_pages, m.x), rf = pool_row(table[m.y / kPagePos], a.n_pages, m.y);
+      if (rt < 0 || rf < 0) continue;
+      uint4* pool = reinterpret_cast<uint4*>(rest < a.row_pieces ? a.k_pool : a.v_pool);
+      to[k] = pool + ((layer_rows + rt) * a.Hkv + h) * a.row_pieces + piece;
+      x[k] = pool[((layer_rows + rf) * a.Hkv + h) * a.row_pieces + piece];
+    }
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) if (to[k]) *to[k] = x[k];
+  }
+}
 
-// A CTA per list (layer, sequence, key head): a radix selection over the weights finds the lightest key that stays, ordered
-// scans list the holes below the budget and the survivors above it, then the rows move.  Sources lie at or above the
-// budget, targets below it: no row is read after it was written, in whatever order they move.
+// Selection, a CTA per list (layer, sequence, key head).  An entry's key is its weight as a number whose unsigned order is the
+// order of eviction (-0 like 0); NaN is 1, below every number; entries that stay whatever their weight (recent ones, where they
+// fit the budget) have all bits set, those that leave whatever theirs (what is not recent, where they do not) have 0.  The
+// border is found bit by bit: a candidate stands if at least `budget` keys are not below it, and ends the search where it is
+// exactly so many.  A candidate costs one barrier (a radix selection with its histograms and scans took 26 us for 522 entries).
+// Ordered scans then list the holes below the budget and the survivors above it.
+//
+// KEPT keys a thread stay in registers: 16 (lists of up to 8192 slots, two CTAs to an SM) or 32; what is behind them is read
+// anew for every candidate.
 constexpr int kEvictThreads = 512;
-__global__ void __launch_bounds__(kEvictThreads) cache_evict_kernel(const __grid_constant__ EvictArgs a) {
-  __shared__ int s_hist[2048], s_warp[2][kEvictThreads / 32], s_pick[2];
+__device__ __forceinline__ unsigned evict_key(float w) { return w != w ? 1u : order_bits(w + 0.f); }
+__device__ __forceinline__ unsigned evict_key_of(unsigned key, bool recent, bool recents_stay) {
+  return recent == recents_stay ? (recent ? 0xffffffffu : 0u) : key;
+}
+template <int KEPT>
+__global__ void __launch_bounds__(kEvictThreads, KEPT <= 16 ? 2 : 1) cache_evict_kernel(const __grid_constant__ EvictArgs a) {
+  constexpr int WARPS = kEvictThreads / 32, SPAN = kEvictThreads * KEPT;
+  __shared__ __align__(16) int s_warp[2][WARPS];
+  __shared__ int s_at[2][KEPT * WARPS], s_sum[2];
+  pdl_launch_dependents();
   const int list = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int h = list % a.Hkv, b = list / a.Hkv % a.B, layer = list / a.Hkv / a.B;
   const int cap = a.ppr * kPagePos, len = clamp_int(a.lens[b], 0, cap);
   if (layer == 0 && h == 0 && tid == 0) a.out_lens[b] = min(len, a.budget);
-  if (len <= a.budget) return;
+  if (len <= a.budget) {
+    if (tid == 0) a.counts[list] = 0;
+    return;
+  }
   float* w = a.weights + (long long)list * cap;
   int* pos = a.positions + (long long)list * cap;
   const long long recent_from = (long long)a.seen[b] - a.recent;
-
-  auto block_count = [&](int v) {                          // sum over the block
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    __syncthreads();
-    if (lane == 0) s_warp[0][warp] = v;
+  int turn = 0;
+  auto total = [&](int v) {                                // sum over the block
+    v = __reduce_add_sync(0xffffffffu, v);
+    int* box = s_warp[turn++ & 1];                         // (alternating: one barrier is enough)
+    if (lane == 0) box[warp] = v;
     __syncthreads();
     int sum = 0;
-    for (int i = 0; i < kEvictThreads / 32; ++i) sum += s_warp[0][i];
+#pragma unroll
+    for (int i = 0; i < WARPS; i += 4) { const int4 x = *reinterpret_cast<const int4*>(box + i); sum += (x.x + x.y) + (x.z + x.w); }
     return sum;
   };
-  int mine = 0;
-  for (int i = tid; i < len; i += kEvictThreads) mine += pos[i] >= recent_from;
-  const int recents = block_count(mine);
-  // the group that the border runs through, and how many of it stay
-  const bool in_recent = recents >= a.budget;
-  int need = in_recent ? a.budget : a.budget - recents;
-  unsigned prefix = 0, prefix_mask = 0;
-  for (int shift = 21; shift >= 0; shift = shift == 21 ? 10 : (shift == 10 ? 0 : -1)) {
-    const int bins = shift == 0 ? 1024 : 2048;
-    for (int i = tid; i < 2048; i += kEvictThreads) s_hist[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < len; i += kEvictThreads) {
-      const unsigned key = evict_key(w[i]);
-      if ((pos[i] >= recent_from) == in_recent && (key & prefix_mask) == prefix) atomicAdd(&s_hist[(key >> shift) & (bins - 1)], 1);
-    }
-    __syncthreads();
-    // the bin, from the heaviest down, in which the count reaches `need`
-    if (warp == 0) {
-      int above = 0;
-      for (int top = bins - 32; top >= 0; top -= 32) {
-        const int n = s_hist[top + 31 - lane];
-        int upto = n;
+  unsigned kept[KEPT], recent = 0;                         // bit k of recent: the entry of turn k is
+  const int turns = (min(len, SPAN) + kEvictThreads - 1) / kEvictThreads;
+  auto load = [&](int base) {
+    recent = 0;
+    float wv[4];
+    int pv[4];
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += x; }
-        const unsigned hit = __ballot_sync(0xffffffffu, above + upto >= need);
-        if (hit) {
-          const int at = __ffs(hit) - 1;
-          if (lane == at) { s_pick[0] = top + 31 - lane; s_pick[1] = need - (above + upto - n); }
-          break;
-        }
-        above += __shfl_sync(0xffffffffu, upto, 31);
+    for (int k0 = 0; k0 < KEPT; k0 += 4) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = base + tid + (k0 + k) * kEvictThreads;
+        wv[k] = i < len ? w[i] : 0.f;
+        pv[k] = i < len ? pos[i] : 0;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        kept[k0 + k] = evict_key(wv[k]);
+        if (base + tid + (k0 + k) * kEvictThreads < len && pv[k] >= recent_from) recent |= 1u << (k0 + k);
       }
     }
-    __syncthreads();
-    prefix |= (unsigned)s_pick[0] << shift;
-    prefix_mask |= (unsigned)(bins - 1) << shift;
-    need = s_pick[1];
-    __syncthreads();
+  };
+  load(0);
+  int mine = __popc(recent);
+  for (int i = SPAN + tid; i < len; i += kEvictThreads) mine += pos[i] >= recent_from;
+  const bool recents_stay = total(mine) < a.budget;
+  auto settle = [&](int base) {                            // what is not there has key 0
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k)
+      kept[k] = base + tid + k * kEvictThreads < len ? evict_key_of(kept[k], (recent >> k) & 1, recents_stay) : 0u;
+  };
+  settle(0);
+  auto count = [&](unsigned x) {                           // keys that are at least x (x > 0)
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k) n += kept[k] >= x;
+    for (int i = SPAN + tid; i < len; i += kEvictThreads) n += evict_key_of(evict_key(w[i]), pos[i] >= recent_from, recents_stay) >= x;
+    return total(n);
+  };
+  unsigned border = 0;
+  bool exact = false;
+  for (int bit = 31; bit >= 0 && !exact; --bit) {
+    const unsigned candidate = border | (1u << bit);
+    const int n = count(candidate);
+    if (n >= a.budget) border = candidate;
+    exact = n == a.budget;
   }
-  // `prefix` is the border's key, `need` how many entries of that key stay (the lowest slots)
-  int* holes = a.moves + (long long)list * 2 * a.moves_cap;
-  int* fill = holes + a.moves_cap;
+  // of the entries equal to the border the lowest slots stay (there is one that leaves: the border is not all bits)
+  const int room = exact ? len : a.budget - count(border + 1);
+  int2* moves = a.moves + (long long)list * a.moves_cap;
   int ties = 0, n_holes = 0, n_fill = 0;
-  for (int i0 = 0; i0 < len; i0 += kEvictThreads) {
-    const int i = i0 + tid;
-    bool stays = false, tie = false;
-    if (i < len) {
-      const bool rec = pos[i] >= recent_from;
-      if (rec != in_recent) stays = rec;
-      else {
-        const unsigned key = evict_key(w[i]);
-        stays = key > prefix;
-        tie = key == prefix;
+  // Entries are numbered in order: the counts of all turns and warps are scanned by one warp, in place.
+  auto scan = [&](int which, int n_turns) {
+    int run = 0;
+    for (int i = lane; i - lane < n_turns * WARPS; i += 32) {
+      const int v = i < n_turns * WARPS ? s_at[which][i] : 0;
+      int upto = v;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += x; }
+      if (i < n_turns * WARPS) s_at[which][i] = run + upto - v;
+      run += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (lane == 0) s_sum[which] = run;
+  };
+  const unsigned before = (1u << lane) - 1;
+  for (int base = 0; base < len; base += SPAN) {
+    if (base > 0) {
+      load(base);
+      settle(base);
+    }
+    const int n_turns = base == 0 ? turns : (min(len - base, SPAN) + kEvictThreads - 1) / kEvictThreads;
+    unsigned stays = 0;                                    // bit k: the entry of turn k
+    if (!exact) {
+#pragma unroll
+      for (int k = 0; k < KEPT; ++k) {
+        if (k >= n_turns) break;
+        const unsigned m = __ballot_sync(0xffffffffu, kept[k] == border && base + tid + k * kEvictThreads < len);
+        if (lane == 0) s_at[0][k * WARPS + warp] = __popc(m);
       }
+      __syncthreads();
+      if (warp == 0) scan(0, n_turns);
+      __syncthreads();
     }
-    unsigned m = __ballot_sync(0xffffffffu, tie);
-    if (lane == 0) s_warp[0][warp] = __popc(m);
-    __syncthreads();
-    int before = ties, all = 0;
-    for (int k = 0; k < kEvictThreads / 32; ++k) { if (k < warp) before += s_warp[0][k]; all += s_warp[0][k]; }
-    if (tie && before + __popc(m & ((1u << lane) - 1)) < need) stays = true;
-    ties += all;
-    const bool hole = i < a.budget && !stays, filler = i < len && i >= a.budget && stays;   // (i < budget < len)
-    const unsigned mh = __ballot_sync(0xffffffffu, hole), mf = __ballot_sync(0xffffffffu, filler);
-    __syncthreads();
-    if (lane == 0) { s_warp[0][warp] = __popc(mh); s_warp[1][warp] = __popc(mf); }
-    __syncthreads();
-    int bh = n_holes, bf = n_fill;
-    for (int k = 0; k < kEvictThreads / 32; ++k) {
-      if (k < warp) { bh += s_warp[0][k]; bf += s_warp[1][k]; }
-      n_holes += s_warp[0][k]; n_fill += s_warp[1][k];
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k) {
+      if (k >= n_turns) break;
+      const bool tie = kept[k] == border && base + tid + k * kEvictThreads < len;
+      const unsigned m = __ballot_sync(0xffffffffu, tie);
+      const bool in = kept[k] > border || (tie && (exact || ties + s_at[0][k * WARPS + warp] + __popc(m & before) < room));
+      if (in) stays |= 1u << k;
     }
-    if (hole) holes[bh + __popc(mh & ((1u << lane) - 1))] = i;
-    if (filler) fill[bf + __popc(mf & ((1u << lane) - 1))] = i;
+    if (!exact) ties += s_sum[0];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k) {
+      if (k >= n_turns) break;
+      const int i = base + tid + k * kEvictThreads;
+      const bool in = (stays >> k) & 1;
+      const unsigned holes = __ballot_sync(0xffffffffu, i < a.budget && !in), fill = __ballot_sync(0xffffffffu, i >= a.budget && in);
+      if (lane == 0) { s_at[0][k * WARPS + warp] = __popc(holes); s_at[1][k * WARPS + warp] = __popc(fill); }
+    }
+    __syncthreads();
+    if (warp < 2) scan(warp, n_turns);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k) {
+      if (k >= n_turns) break;
+      const int i = base + tid + k * kEvictThreads;
+      const bool in = (stays >> k) & 1, hole = i < a.budget && !in, filler = i >= a.budget && in;
+      const unsigned holes = __ballot_sync(0xffffffffu, hole), fill = __ballot_sync(0xffffffffu, filler);
+      if (hole) moves[n_holes + s_at[0][k * WARPS + warp] + __popc(holes & before)].x = i;
+      if (filler) moves[n_fill + s_at[1][k * WARPS + warp] + __popc(fill & before)].y = i;
+    }
+    n_holes += s_sum[0];
+    n_fill += s_sum[1];
     __syncthreads();
   }
-  __threadfence_block();
-  __syncthreads();
+  // (as many of one as of the other: `budget` entries stay)
   const int n = min(n_holes, n_fill);
-  const int* table = a.table + (long long)b * a.ppr;
-  const long long layer_rows = (long long)layer * a.n_pages * kPagePos;
-  for (long long i = tid; i < (long long)n * 2 * a.row_pieces; i += kEvictThreads) {
-    const int j = (int)(i / (2 * a.row_pieces)), rest = (int)(i % (2 * a.row_pieces)), which = rest / a.row_pieces, piece = rest % a.row_pieces;
-    const int to = holes[j], from = fill[j];
-    const long long rt = pool_row(table[to / kPagePos], a.n_pages, to), rf = pool_row(table[from / kPagePos], a.n_pages, from);
-    if (rt < 0 || rf < 0) continue;
-    uint4* pool = reinterpret_cast<uint4*>(which ? a.v_pool : a.k_pool);
-    pool[((layer_rows + rt) * a.Hkv + h) * a.row_pieces + piece] = pool[((layer_rows + rf) * a.Hkv + h) * a.row_pieces + piece];
-  }
+  if (tid == 0) a.counts[list] = n;
+#pragma unroll 4
   for (int j = tid; j < n; j += kEvictThreads) {
-    w[holes[j]] = w[fill[j]];
-    pos[holes[j]] = pos[fill[j]];
+    const int2 m = moves[j];
+    w[m.x] = w[m.y];
+    pos[m.x] = pos[m.y];
   }
+  if (a.move_here) move_rows(a, list, n, tid, kEvictThreads);
+}
+
+// Moves, for lists where they are many: grid (lists, parts).
+constexpr int kMoveThreads = 256;
+__global__ void __launch_bounds__(kMoveThreads) cache_move_kernel(const __grid_constant__ EvictArgs a) {
+  pdl_wait();
+  move_rows(a, blockIdx.x, a.counts[blockIdx.x], (long long)blockIdx.y * kMoveThreads + threadIdx.x, (long long)gridDim.y * kMoveThreads);
 }
 
 // ------------------------------------------------------------------ page means
