@@ -278,16 +278,15 @@ int bpd_op_cache_evict(const bpd_cache* cache, const int32_t* lens, const int32_
   const int lists = a.layers * a.B * a.Hkv;
   a.moves = static_cast<int2*>(scratch); a.moves_cap = moves_cap(cache, budget);
   a.counts = reinterpret_cast<int*>(static_cast<char*>(scratch) + round256((size_t)lists * a.moves_cap * 8));
-  // Up to 128 entries a list move within the launch that selects them (a block over the budget: 522 entries of 48 lists, EVICT1);
-  // more are shared by all SMs in a launch of their own (256 lists of up to 8000: EVICT2).
+  // Up to 128 entries a list move within the launch that selects them (a block over the budget: 522 entries of 48 lists);
+  // more are shared by all SMs in a launch of their own (256 lists of up to 8000: 38 us).
   a.move_here = a.moves_cap <= 128 ? 1 : 0;
   if (a.ppr * kPagePos <= 16 * kEvictThreads) BPD_CUDA(launch_k(cache_evict_kernel<16>, dim3(lists), dim3(kEvictThreads), 0, (cudaStream_t)cuda_stream, false, a));
   else BPD_CUDA(launch_k(cache_evict_kernel<32>, dim3(lists), dim3(kEvictThreads), 0, (cudaStream_t)cuda_stream, false, a));
   ++g_launches;
   if (!a.move_here) {
-    // parts of at least eight turns of a CTA; more of them where lists are few
-    const long long turns = (long long)a.moves_cap * 2 * a.row_pieces / (kMoveThreads * 8) + 1;
-    const int parts = (int)std::max<long long>(1, std::min<long long>(turns, std::max(2, 8 * kSMs / lists)));
+    // a warp for 32 moves
+    const int parts = std::min(ceil_div(a.moves_cap, kMoveThreads), 65535);
     BPD_CUDA(launch_k(cache_move_kernel, dim3(lists, parts), dim3(kMoveThreads), 0, (cudaStream_t)cuda_stream, true, a));
     ++g_launches;
   }
