@@ -129,7 +129,7 @@ int launch_select(SelectArgs& a, int D, cudaStream_t st) {
 
 template <typename CT>
 int launch_weights(const WeightArgs& a, int D, cudaStream_t st) {
-  const dim3 grid(a.B * a.Hkv, ceil_div(a.ppr, kWPages));
+  const dim3 grid((unsigned)std::min<long long>((long long)a.B * a.Hkv * a.ppr, 2 * kSMs));
   BPD_TREE_BY_DIM(BPD_CUDA(launch_k(cache_weights_kernel<CT, DD>, grid, dim3(kWThreads), 0, st, false, a)); break;)
   ++g_launches;
   return BPD_OK;
@@ -249,8 +249,8 @@ int bpd_op_cache_weights(const bpd_cache* cache, const void* q, int nodes, int h
   WeightArgs a;
   a.q = q; a.k_pool = cache->k_pool; a.lse = lse; a.path = path; a.accepted = accepted; a.lens = lens; a.seen = seen;
   a.table = cache->page_table; a.B = cache->batch; a.T = nodes; a.H = heads; a.Hkv = cache->kv_heads; a.G = heads / cache->kv_heads;
-  a.ppr = cache->pages_per_row; a.n_pages = cache->n_pages; a.q_stride = q_stride; a.scale = scale; a.weights = weights; a.positions = positions;
-  if (ceil_div(a.ppr, kWPages) > 65535) return fail(BPD_E_SHAPE, "pages_per_row out of range");
+  a.ppr = cache->pages_per_row; a.n_pages = cache->n_pages; a.q_stride = q_stride; a.scale_log2 = (float)((double)scale * 1.4426950408889634); a.weights = weights; a.positions = positions;
+  if ((long long)a.ppr * a.Hkv > 0x7fffffffLL) return fail(BPD_E_SHAPE, "pages_per_row * kv_heads out of range");
   return cache->dtype == 0 ? launch_weights<float>(a, cache->head_dim, (cudaStream_t)cuda_stream)
                            : launch_weights<bf16>(a, cache->head_dim, (cudaStream_t)cuda_stream);
 }

@@ -1,8 +1,7 @@
 // Operators on a paged cache beside its attention: commit of an accepted path, accumulated attention weights, eviction,
 // page means, selection of pages.
 #pragma once
-#include "attention.cuh"
-#include "cache_index.hpp"
+#include "tree_attention.cuh"
 
 namespace bpd {
 namespace tree {
@@ -90,7 +89,7 @@ struct WeightArgs {
   const int *path, *accepted, *lens, *seen, *table;
   int B, T, H, Hkv, G, ppr, n_pages;
   long long q_stride;
-  float scale;
+  float scale_log2;                    // scale * log2(e)
   float* weights;                      // [B][Hkv][ppr * 64]
   int* positions;
 };
@@ -100,8 +99,9 @@ struct WeightArgs {
 // A product with keys on M and (node, head) rows on N whose result is summed over N: no key depends on another, so a warp
 // streams 16 keys straight from global memory into fragments (the order of the products' k is free as long as both operands
 // agree: a thread takes 16 contiguous bytes) and no key passes through shared memory.  Queries are staged once per CTA.
-// grid (B * Hkv, page groups).  Bound by reading the keys.
-constexpr int kWThreads = 256, kWPages = 8;
+// Pages of all (sequence, key head) pairs are laid end to end and every CTA takes an equal run of them (with 8 pages a CTA, the
+// queries' way into shared memory took as long as the keys).  Bound by reading the keys.
+constexpr int kWThreads = 256;
 template <typename CT, int D>
 struct WShape {
   static constexpr bool F32 = sizeof(CT) == 4;
@@ -116,117 +116,193 @@ __global__ void __launch_bounds__(kWThreads) cache_weights_kernel(const __grid_c
   using W = WShape<CT, D>;
   constexpr int VEC = W::VEC, PL = W::PLANES;
   __shared__ __align__(16) bf16 s_q[PL * W::ROWS * W::QP];
-  __shared__ float s_lse[W::ROWS];
+  __shared__ __align__(8) float s_hi[W::ROWS], s_lo[W::ROWS];      // log2(e) lse in two parts: its rounding would weigh on every weight alike
   __shared__ int s_step[W::ROWS];                                  // index on the path: the row sees positions <= len + it
-  const int b = blockIdx.x / a.Hkv, h = blockIdx.x % a.Hkv, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
-  const int cap = a.ppr * kPagePos, len = clamp_int(a.lens[b], 0, cap);
-  const int got = clamp_int(a.accepted[b], 0, min(a.T, cap - len)), total = len + got;
-  if (got == 0 || blockIdx.y * kWPages * kPagePos >= total) return;
-  const int rows = got * a.G;
-  const int p_end = min(ceil_div(total, kPagePos), (int)(blockIdx.y + 1) * kWPages);
-  float* wout = a.weights + ((long long)b * a.Hkv + h) * cap;
-  int* pout = a.positions + ((long long)b * a.Hkv + h) * cap;
-  for (int r0 = 0; r0 < rows; r0 += W::ROWS) {
-    const int n = min(W::ROWS, rows - r0), n8 = (n + 7) & ~7;
-    __syncthreads();
-    for (int i = tid; i < n8 * (D / 4); i += kWThreads) {
-      const int r = i / (D / 4), c = i % (D / 4) * 4;
-      float v[4] = {0.f, 0.f, 0.f, 0.f};
-      if (r < n) {
-        const int node = clamp_int(a.path[(long long)b * a.T + (r0 + r) / a.G], 0, a.T - 1), head = h * a.G + (r0 + r) % a.G;
-        const CT* src = reinterpret_cast<const CT*>(a.q) + ((long long)b * a.T + node) * a.q_stride + head * D + c;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3, cap = a.ppr * kPagePos;
+  auto length = [&](int b) { return clamp_int(a.lens[b], 0, cap); };
+  auto taken = [&](int b, int len) { return clamp_int(a.accepted[b], 0, min(a.T, cap - len)); };
+  auto pages_of = [&](int b) { const int len = length(b), got = taken(b, len); return got ? ceil_div(len + got, kPagePos) : 0; };
+  // this CTA's run of pages (every warp finds it out alone)
+  long long sum = 0;
+  for (int i = lane; i < a.B; i += 32) sum += (long long)pages_of(i) * a.Hkv;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = to_f(src[e]);
-        if (c == 0) { s_lse[r] = a.lse[((long long)b * a.T + node) * a.H + head]; s_step[r] = (r0 + r) / a.G; }
-      } else if (c == 0) {
-        s_lse[r] = INFINITY; s_step[r] = -1;                       // weight 0
-      }
-      if constexpr (W::F32) {
-        uint32_t x[3], y[3];
-        attn::split3_pair(v[0], v[1], x);
-        attn::split3_pair(v[2], v[3], y);
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  const Runs runs = runs_of(sum, (int)gridDim.x);
+  if ((int)blockIdx.x >= runs.ctas) return;
+  long long u = first_unit(runs, blockIdx.x), seq_first = 0;
+  const long long u_end = first_unit(runs, blockIdx.x + 1);
+  int b = 0;
+  for (int b0 = 0;; b0 += 32) {
+    const long long n = b0 + lane < a.B ? (long long)pages_of(b0 + lane) * a.Hkv : 0;
+    long long upto = n;
 #pragma unroll
-        for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2*>(s_q + (q * W::ROWS + r) * W::QP + c) = make_uint2(x[q], y[q]);
-      } else {
-        *reinterpret_cast<uint2*>(s_q + r * W::QP + c) = make_uint2(attn::pack2(from_f<bf16>(v[0]), from_f<bf16>(v[1])), attn::pack2(from_f<bf16>(v[2]), from_f<bf16>(v[3])));
-      }
+    for (int o = 1; o < 32; o <<= 1) { const long long x = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += x; }
+    const unsigned hit = __ballot_sync(0xffffffffu, seq_first + upto > u);
+    if (hit) {
+      const int at = __ffs(hit) - 1;
+      b = b0 + at;
+      seq_first += __shfl_sync(0xffffffffu, upto - n, at);
+      break;
     }
-    __syncthreads();
-    for (int tile = blockIdx.y * kWPages * 4 + warp; tile < p_end * 4; tile += kWThreads / 32) {
-      const int pos0 = tile * 16;
-      if (pos0 >= total) break;
-      const int page = a.table[(long long)b * a.ppr + pos0 / kPagePos];
-      const long long row = pool_row(page, a.n_pages, pos0);
-      const bool ok[2] = {row >= 0 && pos0 + g < total, row >= 0 && pos0 + g + 8 < total};
-      const CT* kp = reinterpret_cast<const CT*>(a.k_pool) + ((row < 0 ? 0 : row) * a.Hkv + h) * D;
-      float sum0 = 0.f, sum1 = 0.f;
-      uint32_t kf[PL][W::STEPS][2][VEC / 2];                       // [plane][take][row half][pairs]
+    seq_first += __shfl_sync(0xffffffffu, upto, 31);
+  }
+  int pages = pages_of(b);
+  while (u < u_end) {
+    while (u >= seq_first + (long long)pages * a.Hkv) {
+      seq_first += (long long)pages * a.Hkv;
+      pages = pages_of(++b);
+    }
+    const int into = (int)(u - seq_first), h = into / pages, p_begin = into % pages, p_end = (int)min((long long)pages, p_begin + (u_end - u));
+    u += p_end - p_begin;
+    const int len = length(b), got = taken(b, len), total = len + got, rows = got * a.G;
+    float* wout = a.weights + ((long long)b * a.Hkv + h) * cap;
+    int* pout = a.positions + ((long long)b * a.Hkv + h) * cap;
+    for (int r0 = 0; r0 < rows; r0 += W::ROWS) {
+      const int n = min(W::ROWS, rows - r0), n8 = (n + 7) & ~7;
+      __syncthreads();
+      for (int i = tid; i < n8 * (D / 4); i += kWThreads) {
+        const int r = i / (D / 4), c = i % (D / 4) * 4;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        if (r < n) {
+          const int node = clamp_int(a.path[(long long)b * a.T + (r0 + r) / a.G], 0, a.T - 1), head = h * a.G + (r0 + r) % a.G;
+          const CT* src = reinterpret_cast<const CT*>(a.q) + ((long long)b * a.T + node) * a.q_stride + head * D + c;
 #pragma unroll
-      for (int st = 0; st < W::STEPS; ++st)
+          for (int e = 0; e < 4; ++e) v[e] = to_f(src[e]);
+          if (c == 0) {
+            const float lse = a.lse[((long long)b * a.T + node) * a.H + head], hi = lse * 1.44269504f;
+            s_hi[r] = hi;
+            s_lo[r] = fabsf(hi) < INFINITY ? fmaf(lse, 1.44269504f, -hi) + lse * 1.92596299e-8f : 0.f;
+            s_step[r] = (r0 + r) / a.G;
+          }
+        } else if (c == 0) {
+          s_hi[r] = INFINITY; s_lo[r] = 0.f; s_step[r] = -1;         // weight 0
+        }
+        if constexpr (W::F32) {
+          uint32_t x[3], y[3];
+          attn::split3_pair(v[0], v[1], x);
+          attn::split3_pair(v[2], v[3], y);
+#pragma unroll
+          for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2*>(s_q + (q * W::ROWS + r) * W::QP + c) = make_uint2(x[q], y[q]);
+        } else {
+          *reinterpret_cast<uint2*>(s_q + r * W::QP + c) = make_uint2(attn::pack2(from_f<bf16>(v[0]), from_f<bf16>(v[1])), attn::pack2(from_f<bf16>(v[2]), from_f<bf16>(v[3])));
+        }
+      }
+      __syncthreads();
+      // keys of a tile: [take][row half]; 16 (or 8) bytes a take
+      struct Keys { uint32_t v[W::STEPS][2][VEC * (int)sizeof(CT) / 4]; bool ok[2]; };
+      const int t_end = min(p_end * 4, (total + 15) / 16);
+      auto look_up = [&](int tile) { return tile < t_end ? a.table[(long long)b * a.ppr + tile / 4] : -1; };
+      auto fetch = [&](int tile, int page, Keys& k) {
+        const int pos0 = tile * 16;
+        const long long row = pool_row(page, a.n_pages, pos0);
+        const CT* kp = reinterpret_cast<const CT*>(a.k_pool) + ((row < 0 ? 0 : row) * a.Hkv + h) * D;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          const CT* src = kp + (long long)(g + half * 8) * a.Hkv * D + (t4 + 4 * st) * VEC;
-          if constexpr (W::F32) {
-            float4 v[VEC / 4];
+          k.ok[half] = tile < t_end && row >= 0 && pos0 + g + half * 8 < total;
 #pragma unroll
-            for (int e = 0; e < VEC / 4; ++e) v[e] = ok[half] ? reinterpret_cast<const float4*>(src)[e] : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int e = 0; e < VEC / 4; ++e) {
-              uint32_t x[3], y[3];
-              attn::split3_pair(v[e].x, v[e].y, x);
-              attn::split3_pair(v[e].z, v[e].w, y);
-#pragma unroll
-              for (int q = 0; q < PL; ++q) { kf[q][st][half][2 * e] = x[q]; kf[q][st][half][2 * e + 1] = y[q]; }
-            }
-          } else if constexpr (VEC == 8) {
-            const uint4 v = ok[half] ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
-            kf[0][st][half][0] = v.x; kf[0][st][half][1] = v.y; kf[0][st][half][2] = v.z; kf[0][st][half][3] = v.w;
-          } else {
-            const uint2 v = ok[half] ? *reinterpret_cast<const uint2*>(src) : make_uint2(0u, 0u);
-            kf[0][st][half][0] = v.x; kf[0][st][half][1] = v.y;
-          }
-        }
-      for (int n0 = 0; n0 < n8; n0 += 8) {
-        float c[4] = {0.f, 0.f, 0.f, 0.f}, lo[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int st = 0; st < W::STEPS; ++st) {
-          uint32_t qf[PL][VEC / 2];
-#pragma unroll
-          for (int q = 0; q < PL; ++q) {
-            const bf16* src = s_q + (q * W::ROWS + n0 + g) * W::QP + (t4 + 4 * st) * VEC;
-            if constexpr (VEC == 8) {
-              const uint4 v = *reinterpret_cast<const uint4*>(src);
-              qf[q][0] = v.x; qf[q][1] = v.y; qf[q][2] = v.z; qf[q][3] = v.w;
+          for (int st = 0; st < W::STEPS; ++st) {
+            const CT* src = kp + (long long)(g + half * 8) * a.Hkv * D + (t4 + 4 * st) * VEC;
+            constexpr int WORDS = VEC * (int)sizeof(CT) / 4;
+            if constexpr (WORDS == 2) {
+              *reinterpret_cast<uint2*>(k.v[st][half]) = k.ok[half] ? *reinterpret_cast<const uint2*>(src) : make_uint2(0u, 0u);
             } else {
-              const uint2 v = *reinterpret_cast<const uint2*>(src);
-              qf[q][0] = v.x; qf[q][1] = v.y;
+#pragma unroll
+              for (int e = 0; e < WORDS; e += 4)
+                *reinterpret_cast<uint4*>(&k.v[st][half][e]) = k.ok[half] ? reinterpret_cast<const uint4*>(src)[e / 4] : make_uint4(0u, 0u, 0u, 0u);
             }
           }
+        }
+      };
+      auto add_up = [&](int tile, const Keys& keys) {
+        const int pos0 = tile * 16;
+        float sum0 = 0.f, sum1 = 0.f;
+        for (int n0 = 0; n0 < n8; n0 += 8) {
+          float c[4] = {0.f, 0.f, 0.f, 0.f}, lo[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int k = 0; k < VEC / 4; ++k)
+          for (int st = 0; st < W::STEPS; ++st) {
+            uint32_t qf[PL][VEC / 2];
 #pragma unroll
-            for (int p = 0; p < PL; ++p) {
-              const uint32_t aq[4] = {kf[p][st][0][2 * k], kf[p][st][1][2 * k], kf[p][st][0][2 * k + 1], kf[p][st][1][2 * k + 1]};
-#pragma unroll
-              for (int q = 0; q < PL - p; ++q) attn::mma_bf16(p + q == 0 ? c : lo, aq, qf[q][2 * k], qf[q][2 * k + 1]);
+            for (int q = 0; q < PL; ++q) {
+              const bf16* src = s_q + (q * W::ROWS + n0 + g) * W::QP + (t4 + 4 * st) * VEC;
+              if constexpr (VEC == 8) {
+                const uint4 v = *reinterpret_cast<const uint4*>(src);
+                qf[q][0] = v.x; qf[q][1] = v.y; qf[q][2] = v.z; qf[q][3] = v.w;
+              } else {
+                const uint2 v = *reinterpret_cast<const uint2*>(src);
+                qf[q][0] = v.x; qf[q][1] = v.y;
+              }
             }
-        }
+            uint32_t kf[PL][2][VEC / 2];                             // [plane][row half][pairs]
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int r = n0 + t4 * 2 + (j & 1), pos = pos0 + g + (j < 2 ? 0 : 8);
-          const float w = pos <= len + s_step[r] ? expf(fmaf(c[j] + lo[j], a.scale, -s_lse[r])) : 0.f;
-          if (j < 2) sum0 += w; else sum1 += w;
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+              for (int e = 0; e < VEC / 2; ++e) {
+                if constexpr (W::F32) {
+                  uint32_t x[3];
+                  attn::split3_pair(__uint_as_float(keys.v[st][half][2 * e]), __uint_as_float(keys.v[st][half][2 * e + 1]), x);
+#pragma unroll
+                  for (int q = 0; q < PL; ++q) kf[q][half][e] = x[q];
+                } else {
+                  kf[0][half][e] = keys.v[st][half][e];
+                }
+              }
+#pragma unroll
+            for (int k = 0; k < VEC / 4; ++k)
+#pragma unroll
+              for (int p = 0; p < PL; ++p) {
+                const uint32_t aq[4] = {kf[p][0][2 * k], kf[p][1][2 * k], kf[p][0][2 * k + 1], kf[p][1][2 * k + 1]};
+#pragma unroll
+                for (int q = 0; q < PL - p; ++q) attn::mma_bf16(p + q == 0 ? c : lo, aq, qf[q][2 * k], qf[q][2 * k + 1]);
+              }
+          }
+          const float2 hi = *reinterpret_cast<const float2*>(s_hi + n0 + t4 * 2), low = *reinterpret_cast<const float2*>(s_lo + n0 + t4 * 2);
+          float e[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) e[j] = exp2_fast(fmaf(c[j] + lo[j], a.scale_log2, -(j & 1 ? hi.y : hi.x)) - (j & 1 ? low.y : low.x));
+          if (pos0 + 16 > len) {                                   // entries of this commit: rows before them do not see them
+            const int pos = pos0 + g, step0 = s_step[n0 + t4 * 2], step1 = s_step[n0 + t4 * 2 + 1];
+            if (pos > len + step0) e[0] = 0.f;
+            if (pos > len + step1) e[1] = 0.f;
+            if (pos + 8 > len + step0) e[2] = 0.f;
+            if (pos + 8 > len + step1) e[3] = 0.f;
+          }
+          sum0 += e[0] + e[1];
+          sum1 += e[2] + e[3];
         }
-      }
-      sum0 += __shfl_xor_sync(0xffffffffu, sum0, 1); sum0 += __shfl_xor_sync(0xffffffffu, sum0, 2);
-      sum1 += __shfl_xor_sync(0xffffffffu, sum1, 1); sum1 += __shfl_xor_sync(0xffffffffu, sum1, 2);
-      if (t4 < 2) {
-        const int pos = pos0 + g + t4 * 8;
-        const float add = t4 ? sum1 : sum0;
-        if (pos < total) {
-          // entries of this commit begin here: nothing of what the slot held before counts
-          wout[pos] = (pos < len || r0 > 0) ? wout[pos] + (ok[t4] ? add : 0.f) : (ok[t4] ? add : 0.f);
-          if (pos >= len && r0 == 0) pout[pos] = a.seen[b] + pos - len;
+        sum0 += __shfl_xor_sync(0xffffffffu, sum0, 1); sum0 += __shfl_xor_sync(0xffffffffu, sum0, 2);
+        sum1 += __shfl_xor_sync(0xffffffffu, sum1, 1); sum1 += __shfl_xor_sync(0xffffffffu, sum1, 2);
+        if (t4 < 2) {
+          const int pos = pos0 + g + t4 * 8;
+          const float add = t4 ? (keys.ok[1] ? sum1 : 0.f) : (keys.ok[0] ? sum0 : 0.f);
+          if (pos < total) {
+            // entries of this commit begin here: nothing of what the slot held before counts
+            wout[pos] = pos < len || r0 > 0 ? wout[pos] + add : add;
+            if (pos >= len && r0 == 0) pout[pos] = a.seen[b] + pos - len;
+          }
+        }
+      };
+      constexpr int STEP = kWThreads / 32;
+      int tile = p_begin * 4 + warp, page = look_up(tile);
+      if constexpr (W::F32) {
+        for (; tile < t_end; tile += STEP) {
+          const int next = look_up(tile + STEP);
+          Keys k;
+          fetch(tile, page, k);
+          add_up(tile, k);
+          page = next;
+        }
+      } else {
+        // one tile's keys are on their way while the other's are used
+        Keys k0, k1;
+        fetch(tile, page, k0);
+        page = look_up(tile + STEP);
+        for (; tile < t_end; tile += 2 * STEP) {
+          fetch(tile + STEP, page, k1);
+          page = look_up(tile + 2 * STEP);
+          add_up(tile, k0);
+          fetch(tile + 2 * STEP, page, k0);
+          page = look_up(tile + 3 * STEP);
+          if (tile + STEP < t_end) add_up(tile + STEP, k1);
         }
       }
     }

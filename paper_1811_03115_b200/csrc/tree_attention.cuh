@@ -34,6 +34,13 @@ constexpr int kThreads = 128;
 constexpr int kPagesAhead = 64;   // pages looked up at a time
 constexpr int kChunk = kPagePos;
 
+// 2 units of error, 0 below the smallest normal number.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 struct AttnArgs {
   const void *q, *k_new, *v_new, *k_pool, *v_pool;
   const int *table, *lens, *parents, *nodes;   // nodes may be null: T each

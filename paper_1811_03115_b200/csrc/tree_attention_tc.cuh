@@ -87,11 +87,6 @@ __device__ __forceinline__ uint64_t value_desc(uint32_t saddr, int panel_bytes) 
   d |= (uint64_t)2 << 61;
   return d;
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 
 template <int D, bool PAGED>
 __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ TcMaps maps) {
