@@ -315,7 +315,8 @@ int bpd_op_linear(const void* x, const void* w, const void* bias, int rows, int 
  * All of these calls only enqueue work on cuda_stream: they may be captured into
  * a graph, and keep nothing between calls.  A scratch belongs to one call until
  * that call's kernels are done (calls on one stream may share one if they are
- * enqueued one after the other).  Kernels trust no value in a device array: a
+ * enqueued one after the other); a scratch_bytes call answers 0 where none is
+ * needed, and for arguments that the call itself refuses.  Kernels trust no value in a device array: a
  * length outside [0, capacity] is clamped to it, a node count to [0, nodes], a
  * parent that does not lie before its node is taken as -1, and a page outside
  * [0, n_pages) is no page: its positions count as masked and are not written.

@@ -474,10 +474,11 @@ def _enqueue(device: int, fn, *args):
 
 
 def _scratch(like, n: int):
-    """n bytes on a tensor's device; 0 is the refusal of the scratch_bytes call that answered it."""
+    """A tensor of n bytes on a tensor's device, and its address; 0 bytes: none is needed, or the call will refuse its arguments."""
     if n == 0:
-        raise BpdError(-2, lib.bpd_last_error().decode(errors="replace"))
-    return like.new_empty(n, dtype=torch.uint8)
+        return None, None
+    t = like.new_empty(n, dtype=torch.uint8)
+    return t, t.data_ptr()
 
 
 def _drafted(cache, q, k_new, v_new, lens, parents, nodes):
@@ -507,9 +508,9 @@ def bpd_op_tree_attention(q, k_new, v_new, k_pool, v_pool, page_table, lens, par
     args = _drafted(cache, q, k_new, v_new, lens, parents, nodes)
     c = C.byref(cache[0])
     n = lib.bpd_op_tree_attention_scratch_bytes(c, args[3], args[4])
-    scratch, out = _scratch(q, n), q.new_empty(*q.shape)
+    (scratch, at), out = _scratch(q, n), q.new_empty(*q.shape)
     lse = q.new_empty(*q.shape[:3], dtype=torch.float32) if want_lse else None
-    _enqueue(cache[3], lib.bpd_op_tree_attention, c, *args, q.shape[3] ** -0.5 if scale is None else scale, scratch.data_ptr(), n, out.data_ptr(),
+    _enqueue(cache[3], lib.bpd_op_tree_attention, c, *args, q.shape[3] ** -0.5 if scale is None else scale, at, n, out.data_ptr(),
              lse.data_ptr() if want_lse else None)
     return (out, lse) if want_lse else out
 
@@ -527,10 +528,10 @@ def bpd_op_page_attention(q, k_new, v_new, k_pool, v_pool, page_table, means, le
     n_sel = min(select, per_row)
     c = C.byref(cache[0])
     n = lib.bpd_op_page_attention_scratch_bytes(c, t, args[4], n_sel)
-    scratch, out = _scratch(q, n), q.new_empty(*q.shape)
+    (scratch, at), out = _scratch(q, n), q.new_empty(*q.shape)
     lse = q.new_empty(*q.shape[:3], dtype=torch.float32) if want_lse else None
     pages = lens.new_empty(b, t, hk, n_sel) if want_pages else None
-    _enqueue(cache[3], lib.bpd_op_page_attention, c, mp, *args, n_sel, d ** -0.5 if scale is None else scale, scratch.data_ptr(), n, out.data_ptr(),
+    _enqueue(cache[3], lib.bpd_op_page_attention, c, mp, *args, n_sel, d ** -0.5 if scale is None else scale, at, n, out.data_ptr(),
              lse.data_ptr() if want_lse else None, pages.data_ptr() if want_pages else None)
     if want_pages and n_sel < select:
         pages = torch.nn.functional.pad(pages, (0, select - n_sel), value=-1)
@@ -586,8 +587,8 @@ def bpd_op_cache_evict(weights, positions, k_pool, v_pool, page_table, lens, see
     lp, sp = _expect(lens, "lens", (b,), i32, device), _expect(seen, "seen", (b,), i32, device)
     ref = C.byref(c)
     n = lib.bpd_op_cache_evict_scratch_bytes(ref, budget)
-    scratch, out = _scratch(weights, n), lens.new_empty(b)
-    _enqueue(device, lib.bpd_op_cache_evict, ref, lp, sp, budget, recent, wp, pp, scratch.data_ptr(), n, out.data_ptr())
+    (scratch, at), out = _scratch(weights, n), lens.new_empty(b)
+    _enqueue(device, lib.bpd_op_cache_evict, ref, lp, sp, budget, recent, wp, pp, at, n, out.data_ptr())
     return out
 
 

@@ -102,6 +102,7 @@ int check_attention(const bpd_cache* c, const void* q, const void* k_new, const 
 int moves_cap(const bpd_cache* c, int budget) { return std::max(1, std::min(budget, c->pages_per_row * kPagePos - std::min(budget, c->pages_per_row * kPagePos))); }
 
 int check_scratch(const void* scratch, size_t have, size_t need) {
+  if (need == 0) return BPD_OK;
   if (!scratch || !aligned(scratch, 256)) return fail(BPD_E_INVALID, "scratch is null or misaligned");
   if (have < need) return fail(BPD_E_NOMEM, "scratch too small: %zu bytes, %zu needed", have, need);
   return BPD_OK;

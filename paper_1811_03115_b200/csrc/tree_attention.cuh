@@ -358,7 +358,7 @@ __device__ __forceinline__ void clear_dead_rows(const AttnArgs& a, int D) {
 // copies, half of the loop's instructions were addresses; TMA's tensor maps cost the host a few microseconds a call, so small
 // calls do without.
 template <typename CT, int D, int WR, bool PAGED, bool TMA>
-__global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ TcMaps maps) {
+__global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tree_attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ TcMaps maps) {
   using S = Shape<CT, D, WR>;
   using L = Rows<CT, D>;
   pdl_launch_dependents();
@@ -472,13 +472,6 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
         }
       }
     }
-    // the rows' lines in the tree, where the run reaches it
-    if (c_end > cache_chunks && lines_of != b) {
-      __syncthreads();                                      // (those of the sequence before have been used)
-      if (warp == 0) find_lines(s_lines, a.parents + (long long)b * a.T, sq.nodes, lane);   // (a barrier follows: look_up's)
-      lines_of = b;
-    }
-
     float o[DT][4];
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
@@ -489,6 +482,11 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
     for (int s = 0; s < S::STAGES - 1; ++s) {
       if (c_begin + s < c_end) load(c_begin + s, (n + s) % S::STAGES);
       if (!TMA) asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    // the nodes' lines, where the run reaches the tree (the loop's barrier follows; those of the sequence before have been used)
+    if (c_end > cache_chunks && lines_of != b) {
+      if (warp == 0) find_lines(s_lines, a.parents + (long long)b * a.T, sq.nodes, lane);
+      lines_of = b;
     }
     for (int c = c_begin; c < c_end; ++c, ++n) {
       const int stage = n % S::STAGES;
@@ -609,12 +607,11 @@ __global__ void __launch_bounds__(kThreads) tree_attention_kernel(const __grid_c
       bool odd = false;
       if (c >= cache_chunks) {
         int bad = 0;
-        for (int i = tid; i < kChunk * D; i += kThreads) {
-          const int r = i / D, d = i % D;
-          float x;
-          if (F32) x = *reinterpret_cast<const float*>(vb + (r * L::VP + d) * 4);
-          else x = __bfloat162float(*reinterpret_cast<const bf16*>(vb + L::swz(r, d / 8) + (d % 8) * 2));
-          bad |= !(fabsf(x) <= 3.402823466e38f);
+        for (int i = tid; i < n_keys * L::PIECES; i += kThreads) {
+          const uint4 v = *reinterpret_cast<const uint4*>(vb + L::v_at(i / L::PIECES, i % L::PIECES));
+          const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) bad |= (x[e] & 0x7f800000u) == 0x7f800000u || (!F32 && (x[e] & 0x7f80u) == 0x7f80u);
         }
         odd = __syncthreads_or(bad) != 0;
       }

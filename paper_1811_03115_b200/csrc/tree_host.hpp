@@ -27,7 +27,7 @@ long long max_chunks(const AttnArgs& a) { return (PAGED ? std::min(a.select, a.p
 inline void scratch_of(int D, AttnPlan* p) {
   const size_t part = (size_t)p->ctas * 2 * part_floats(p->combine_rows, D) * 4;
   p->part_bytes = p->split ? (part + 255) / 256 * 256 : 0;
-  p->info_bytes = p->split ? ((size_t)p->tiles * sizeof(int2) + 255) / 256 * 256 : 256;
+  p->info_bytes = p->split ? ((size_t)p->tiles * sizeof(int2) + 255) / 256 * 256 : 0;
 }
 
 template <typename CT, int D, int WR, bool PAGED>

@@ -27,7 +27,7 @@ P = 0x10000        # an aligned address that no refused call may look at
 
 
 def _cache(b, **over):
-    c = b.bpd_cache(P, P, P, 2, 10, 5, 2, 2, 64, 1)
+    c = b.bpd_cache(P, P, P, 2, 10, 50, 2, 2, 64, 1)
     for name, value in over.items():
         setattr(c, name, value)
     return C.byref(c)
@@ -102,8 +102,8 @@ def test_attention_refuses(b, call):
 
 
 def test_page_attention_refuses_selections(b):
-    assert _paged(b, select=0) == SHAPE and _paged(b, select=6) == SHAPE and _paged(b, means=None) == INVALID and _paged(b, means=P + 4) == INVALID
-    assert b.lib.bpd_op_page_attention_scratch_bytes(_cache(b), 4, 4, 6) == 0
+    assert _paged(b, select=0) == SHAPE and _paged(b, select=51) == SHAPE and _paged(b, means=None) == INVALID and _paged(b, means=P + 4) == INVALID
+    assert b.lib.bpd_op_page_attention_scratch_bytes(_cache(b), 4, 4, 51) == 0
 
 
 def test_commit_weights_and_eviction_refuse(b):
@@ -125,9 +125,10 @@ def test_commit_weights_and_eviction_refuse(b):
 
 def test_scratch_grows_with_what_needs_it(b):
     n = b.lib.bpd_op_tree_attention_scratch_bytes(_cache(b), 4, 4)
-    assert 0 < n < b.lib.bpd_op_tree_attention_scratch_bytes(_cache(b, batch=640, pages_per_row=50), 64, 4)
+    assert 0 < n < b.lib.bpd_op_tree_attention_scratch_bytes(_cache(b, batch=640), 64, 4)
+    assert b.lib.bpd_op_tree_attention_scratch_bytes(_cache(b, pages_per_row=2), 4, 4) == 0          # whole tiles, nothing to join
     assert b.lib.bpd_op_tree_attention_scratch_bytes(_cache(b, head_dim=7), 4, 4) == 0
-    assert b.lib.bpd_op_cache_evict_scratch_bytes(_cache(b), 10 ** 9) == b.lib.bpd_op_cache_evict_scratch_bytes(_cache(b), 320)
+    assert b.lib.bpd_op_cache_evict_scratch_bytes(_cache(b), 10 ** 9) == b.lib.bpd_op_cache_evict_scratch_bytes(_cache(b), 3200)
 
 
 def test_binding_refuses_tensors(b):
