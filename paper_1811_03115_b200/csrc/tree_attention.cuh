@@ -520,27 +520,39 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
 #pragma unroll
       for (int i = 0; i < NT; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
       if constexpr (F32) {
+        // Products one behind the other go to different accumulators (J tiles of keys side by side): a chain on one of them
+        // would wait for every product's latency (64 rows, heads of 64: 202 us instead of 156 over 8 sequences of 4000).
+        constexpr int J = NT < 4 ? NT : 4;
+        float lo[NT][4];                                    // the smaller products
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          float lo[4] = {0.f, 0.f, 0.f, 0.f};               // the smaller products
+        for (int i = 0; i < NT; ++i) lo[i][0] = lo[i][1] = lo[i][2] = lo[i][3] = 0.f;
 #pragma unroll 2
-          for (int k = 0; k < KT; ++k) {
-            const float* kr = reinterpret_cast<const float*>(kb) + (key0 + i * 8 + g) * L::KP + k * 16 + t4 * 2;
-            const float2 x = *reinterpret_cast<const float2*>(kr), y = *reinterpret_cast<const float2*>(kr + 8);
-            uint32_t b0[3], b1[3];
-            split3_pair(x.x, x.y, b0);
-            split3_pair(y.x, y.y, b1);
+        for (int k = 0; k < KT; ++k) {
+          uint32_t aq[3][4];
 #pragma unroll
-            for (int q = 0; q < 3; ++q) {
-              uint32_t aq[4];
-              ldsm4(s_addr(qs + (q * R + wr * 16 + (lane & 15)) * S::QP + k * 16 + (lane >> 4) * 8), aq);
+          for (int q = 0; q < 3; ++q) ldsm4(s_addr(qs + (q * R + wr * 16 + (lane & 15)) * S::QP + k * 16 + (lane >> 4) * 8), aq[q]);
 #pragma unroll
-              for (int p = 0; p < 3 - q; ++p) mma_bf16(p + q == 0 ? s[i] : lo, aq, b0[p], b1[p]);
+          for (int i0 = 0; i0 < NT; i0 += J) {
+            uint32_t b0[J][3], b1[J][3];
+#pragma unroll
+            for (int i = 0; i < J; ++i) {
+              const float* kr = reinterpret_cast<const float*>(kb) + (key0 + (i0 + i) * 8 + g) * L::KP + k * 16 + t4 * 2;
+              const float2 x = *reinterpret_cast<const float2*>(kr), y = *reinterpret_cast<const float2*>(kr + 8);
+              split3_pair(x.x, x.y, b0[i]);
+              split3_pair(y.x, y.y, b1[i]);
             }
-          }
 #pragma unroll
-          for (int j = 0; j < 4; ++j) s[i][j] += lo[j];
+            for (int q = 0; q < 3; ++q)
+#pragma unroll
+              for (int p = 0; p < 3 - q; ++p)
+#pragma unroll
+                for (int i = 0; i < J; ++i) mma_bf16(p + q == 0 ? s[i0 + i] : lo[i0 + i], aq[q], b0[i][p], b1[i][p]);
+          }
         }
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[i][j] += lo[i][j];
       } else {
 #pragma unroll
         for (int k = 0; k < KT; ++k) {
@@ -638,28 +650,45 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
               }
           }
       } else if constexpr (F32) {
+        uint32_t wp[NT / 2][4][3];                          // the weights' planes, once for all columns
 #pragma unroll
-        for (int n = 0; n < DT; ++n) {
-          float acc[4] = {0.f, 0.f, 0.f, 0.f}, lo[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < NT / 2; ++k) {
+          split3_pair(s[2 * k][0], s[2 * k][1], wp[k][0]);
+          split3_pair(s[2 * k][2], s[2 * k][3], wp[k][1]);
+          split3_pair(s[2 * k + 1][0], s[2 * k + 1][1], wp[k][2]);
+          split3_pair(s[2 * k + 1][2], s[2 * k + 1][3], wp[k][3]);
+        }
+        constexpr int J = DT < 4 ? DT : 4;
+#pragma unroll
+        for (int n0 = 0; n0 < DT; n0 += J) {
+          float acc[J][4], lo[J][4];
+#pragma unroll
+          for (int n = 0; n < J; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[n][e] = lo[n][e] = 0.f;
 #pragma unroll
           for (int k = 0; k < NT / 2; ++k) {
-            const float* vr = reinterpret_cast<const float*>(vb) + (key0 + k * 16 + t4 * 2) * L::VP + n * 8 + g;
-            uint32_t b0[3], b1[3], w[4][3];
-            split3_pair(vr[0], vr[L::VP], b0);
-            split3_pair(vr[8 * L::VP], vr[9 * L::VP], b1);
-            split3_pair(s[2 * k][0], s[2 * k][1], w[0]);
-            split3_pair(s[2 * k][2], s[2 * k][3], w[1]);
-            split3_pair(s[2 * k + 1][0], s[2 * k + 1][1], w[2]);
-            split3_pair(s[2 * k + 1][2], s[2 * k + 1][3], w[3]);
+            uint32_t b0[J][3], b1[J][3];
+#pragma unroll
+            for (int n = 0; n < J; ++n) {
+              const float* vr = reinterpret_cast<const float*>(vb) + (key0 + k * 16 + t4 * 2) * L::VP + (n0 + n) * 8 + g;
+              split3_pair(vr[0], vr[L::VP], b0[n]);
+              split3_pair(vr[8 * L::VP], vr[9 * L::VP], b1[n]);
+            }
 #pragma unroll
             for (int q = 0; q < 3; ++q) {
-              const uint32_t ap[4] = {w[0][q], w[1][q], w[2][q], w[3][q]};
+              const uint32_t ap[4] = {wp[k][0][q], wp[k][1][q], wp[k][2][q], wp[k][3][q]};
 #pragma unroll
-              for (int p = 0; p < 3 - q; ++p) mma_bf16(p + q == 0 ? acc : lo, ap, b0[p], b1[p]);
+              for (int p = 0; p < 3 - q; ++p)
+#pragma unroll
+                for (int n = 0; n < J; ++n) mma_bf16(p + q == 0 ? acc[n] : lo[n], ap, b0[n][p], b1[n][p]);
             }
           }
-          o[n][0] = fmaf(o[n][0], f0, acc[0] + lo[0]); o[n][1] = fmaf(o[n][1], f0, acc[1] + lo[1]);
-          o[n][2] = fmaf(o[n][2], f1, acc[2] + lo[2]); o[n][3] = fmaf(o[n][3], f1, acc[3] + lo[3]);
+#pragma unroll
+          for (int n = 0; n < J; ++n) {
+            o[n0 + n][0] = fmaf(o[n0 + n][0], f0, acc[n][0] + lo[n][0]); o[n0 + n][1] = fmaf(o[n0 + n][1], f0, acc[n][1] + lo[n][1]);
+            o[n0 + n][2] = fmaf(o[n0 + n][2], f1, acc[n][2] + lo[n][2]); o[n0 + n][3] = fmaf(o[n0 + n][3], f1, acc[n][3] + lo[n][3]);
+          }
         }
       } else {
 #pragma unroll
