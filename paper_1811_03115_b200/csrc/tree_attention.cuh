@@ -116,10 +116,10 @@ struct Shape {
   static constexpr int Q_BYTES = F32 ? 3 * R * QP * 2 : 0;
   static constexpr int MP = D + 4;                          // pitch of the merge buffer (floats)
   static constexpr int MERGE = WK * R * MP * 4;
-  static constexpr int STAGES = F32 ? (D >= 128 ? 2 : 3) : (D >= 128 ? 3 : 4);
+  static constexpr int STAGES = F32 ? (D >= 64 ? 2 : 3) : (D >= 128 ? 3 : 4);
   static constexpr int RING = STAGES * Rows<CT, D>::STAGE;
   static constexpr int SMEM = 1024 + Q_BYTES + (RING > MERGE ? RING : MERGE);   // (TMA's tiles begin at multiples of 1024)
-  static constexpr int CTAS_PER_SM = F32 ? (D >= 128 ? 1 : 2) : (D >= 128 ? 2 : 3);
+  static constexpr int CTAS_PER_SM = F32 ? (D >= 128 ? 1 : (WR < 4 ? 3 : 2)) : (D >= 128 ? 2 : 3);
 };
 
 // The nodes' lines as bits: bits[word][t] has those of node t's line among nodes 64 * word ..  By doubling: a node takes over
