@@ -82,6 +82,7 @@ int attend(const bpd_cache* c, const void* q, const void* k_new, const void* v_n
   a.part = reinterpret_cast<float*>(scratch);
   a.info = reinterpret_cast<int2*>(scratch + plan.part_bytes);
   a.split = plan.split;
+  a.end_units = plan.end_units;
   a.part_rows = plan.combine_rows;
   a.ctas = plan.ctas;
   return c->dtype == 0 ? launch_attention<float>(a, paged, c->head_dim, plan, st) : launch_attention<bf16>(a, paged, c->head_dim, plan, st);

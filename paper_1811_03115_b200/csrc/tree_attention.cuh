@@ -51,6 +51,7 @@ struct AttnArgs {
   void* out;                                   // [B][T][H][D]
   float* lse;                                  // [B][T][H] or null
   float* part;                                 // [ctas][2][R * (D + 2)]
+  int end_units;                               // what the end of a tile costs, in chunks
   int split;                                   // 1: equal runs of chunks, joined by combine_kernel; 0: a tile per CTA
   int part_rows;                               // rows of a partial result
   int ctas;                                    // CTAs of the launch
@@ -233,7 +234,7 @@ struct Walk {
   const AttnArgs& a;
   const int tile_rows;
   Runs runs;
-  long long u_begin, u, u_end, seq_first;
+  long long u_begin, u, u_end, seq_first, tile_first;
   int b;
   Seq sq;
   Tile tl;
@@ -243,7 +244,7 @@ struct Walk {
   __device__ __forceinline__ Walk(const AttnArgs& args, int rows) : a(args), tile_rows(rows) {}
   __device__ __forceinline__ long long units_of(int i) const {
     const SeqWork w = seq_of<PAGED>(a, i, tile_rows).w;
-    return (long long)w.tiles * w.chunks;
+    return (long long)w.tiles * (w.chunks + a.end_units);
   }
   // False if there is nothing for this CTA.
   __device__ __forceinline__ bool begin() {
@@ -288,24 +289,28 @@ struct Walk {
     }
     sq = seq_of<PAGED>(a, b, tile_rows);
     find();
-    return true;
+    return c_begin < c_end || next();
   }
   // The next tile; false if the CTA's run is done.
   __device__ __forceinline__ bool next() {
     if (!a.split) return false;
-    u += c_end - c_begin;
-    if (u >= u_end) return false;
-    while (u >= seq_first + (long long)sq.w.tiles * sq.w.chunks) {
-      seq_first += (long long)sq.w.tiles * sq.w.chunks;
-      sq = seq_of<PAGED>(a, ++b, tile_rows);
-    }
-    find();
+    do {
+      u = tile_first + sq.w.chunks + a.end_units;
+      if (u >= u_end) return false;
+      while (u >= seq_first + (long long)sq.w.tiles * (sq.w.chunks + a.end_units)) {
+        seq_first += (long long)sq.w.tiles * (sq.w.chunks + a.end_units);
+        sq = seq_of<PAGED>(a, ++b, tile_rows);
+      }
+      find();
+    } while (c_begin >= c_end);
     return true;
   }
+  // The tile that unit u lies in.  (Its chunks' units come first; a run may have nothing but those of its end.)
   __device__ __forceinline__ void find() {
+    const int span = sq.w.chunks + a.end_units;
     const long long into = u - seq_first;
-    const int local = into <= 0x7fffffffLL ? (int)((unsigned)into / (unsigned)sq.w.chunks) : (int)(into / sq.w.chunks);
-    const long long tile_first = seq_first + (long long)local * sq.w.chunks;
+    const int local = into <= 0x7fffffffLL ? (int)((unsigned)into / (unsigned)span) : (int)(into / span);
+    tile_first = seq_first + (long long)local * span;
     c_begin = (int)(u - tile_first);
     c_end = (int)min((long long)sq.w.chunks, u_end - tile_first);
     tl = tile_of<PAGED>(a, b, sq.nodes, local, tile_rows);

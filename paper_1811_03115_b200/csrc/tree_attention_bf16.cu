@@ -21,6 +21,7 @@ int plan_tc(const AttnArgs& a, AttnPlan* p) {
   p->tiles = (int)tiles;
   p->ctas = (int)std::min<long long>(tiles * max_chunks<PAGED>(a), (long long)kSMs * TcShape<D>::CTAS_PER_SM);
   p->combine_rows = std::min(kTcRows, PAGED ? a.G : a.T * a.G);
+  p->end_units = end_units_of(tiles * max_chunks<PAGED>(a), (long long)kSMs * TcShape<D>::CTAS_PER_SM, 8);
   scratch_of(D, p);
   return BPD_OK;
 }
