@@ -313,7 +313,8 @@ int bpd_op_linear(const void* x, const void* w, const void* bias, int rows, int 
  * layer, one page table for all layers.
  *
  * All of these calls only enqueue work on cuda_stream: they may be captured into
- * a graph, and keep nothing between calls.  A scratch belongs to one call until
+ * a graph (after one call of the kind outside of any capture, which loads the
+ * kernels), and keep nothing between calls.  A scratch belongs to one call until
  * that call's kernels are done (calls on one stream may share one if they are
  * enqueued one after the other); a scratch_bytes call answers 0 where none is
  * needed, and for arguments that the call itself refuses.  Kernels trust no value in a device array: a
@@ -348,7 +349,7 @@ typedef struct {
  * boundaries).  They are not written to the cache: bpd_op_tree_commit does that
  * for the accepted ones.  n_nodes: device [batch] or NULL: row b has the first
  * n_nodes[b] nodes; behind them the outputs are 0 and lse is -inf.  1 <= nodes
- * <= 256.  out: device [batch][nodes][heads][head_dim] of dtype.  lse: device
+ * <= 256, scale > 0.  out: device [batch][nodes][heads][head_dim] of dtype.  lse: device
  * float [batch][nodes][heads] or NULL: log of the softmax's sum. */
 size_t bpd_op_tree_attention_scratch_bytes(const bpd_cache* cache, int nodes, int heads);
 int bpd_op_tree_attention(const bpd_cache* cache, const void* q, const void* k_new, const void* v_new, int nodes, int heads,

@@ -156,7 +156,8 @@ def evict(weights, positions, k_pool, v_pool, table, lens, seen, budget, recent)
                 def rank(s):
                     return (p[s] < seen[b] - recent, np.isnan(w[s]), -w[s] if w[s] == w[s] else 0.0, s)
                 kept = sorted(sorted(range(lens[b]), key=rank)[:budget])
-                holes = [s for s in range(budget) if s not in set(kept)]
+                stays = set(kept)
+                holes = [s for s in range(budget) if s not in stays]
                 for to, source in zip(holes, [s for s in kept if s >= budget]):
                     w[to], p[to] = w[source], p[source]
                     for pool in (k_pool, v_pool):

@@ -111,10 +111,11 @@ int check_scratch(const void* scratch, size_t have, size_t need) {
 
 template <typename CT>
 int launch_select(SelectArgs& a, int D, cudaStream_t st) {
-  const long long items = (long long)a.B * a.T * a.Hkv;
+  const bool several = a.T > 1;
+  const long long items = (long long)a.B * (several ? ceil_div(a.T, kSelectNodes) : a.T) * a.Hkv;
   // CTAs for every SM; a share of at least 64 pages each
   a.cluster = 1;
-  while (a.cluster < 8 && items * a.cluster * 2 <= kSMs && a.ppr >= a.cluster * 128) a.cluster *= 2;
+  while (a.cluster < 8 && items * a.cluster * 2 <= 2 * kSMs && a.ppr >= a.cluster * 128) a.cluster *= 2;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
   cfg.gridDim = dim3((unsigned)(items * a.cluster)); cfg.blockDim = dim3(kSelectThreads); cfg.stream = st;
@@ -124,7 +125,7 @@ int launch_select(SelectArgs& a, int D, cudaStream_t st) {
   cfg.attrs = attr;
   cfg.numAttrs = a.cluster > 1 ? 1 : 0;
   void* ptrs[] = {&a};
-  BPD_TREE_BY_DIM(BPD_CUDA(cudaLaunchKernelExC(&cfg, reinterpret_cast<const void*>(page_select_kernel<CT, DD>), ptrs)); break;)
+  BPD_TREE_BY_DIM(BPD_CUDA(cudaLaunchKernelExC(&cfg, several ? reinterpret_cast<const void*>(page_select_nodes_kernel<CT, DD>) : reinterpret_cast<const void*>(page_select_kernel<CT, DD>), ptrs)); break;)
   ++g_launches;
   return BPD_OK;
 }

@@ -621,7 +621,7 @@ struct SelectArgs {
 // score(page) = (sum of the group's queries) . mean, in 64 bits: the border of a selection is often close.  The best
 // `select` full pages (ties and NaN: the lower page, NaN below everything), listed in ascending order.
 //
-// A cluster per (node, key head): its CTAs score a share of the pages each -- a warp takes eight pages at a time and adds up
+// For one node a sequence: a cluster per key head.  Its CTAs score a share of the pages each -- a warp takes eight pages at a time and adds up
 // their eight sums together -- and the first one finds the border bit by bit, from the top: a candidate stands if at least
 // `select` keys are not below it, and ends the search where it is exactly so many.  A candidate costs one barrier that counts
 // (the scores of a sequence differ in their first bits, so some 20 candidates do); histograms of digits, with their atomics
@@ -762,6 +762,133 @@ __global__ void __launch_bounds__(kSelectThreads) page_select_kernel(const __gri
     for (int i = 0; i < WARPS; ++i) { if (i < warp) at += s_warp[i]; done += s_warp[i]; }
     at += __popc(m & ((1u << lane) - 1));
     if (in && at < a.select) out[at] = p;
+  }
+}
+
+// The same for several nodes: a cluster per (key head, four nodes).  The means are read once for the four (each node
+// for itself, 512 selections among 540 pages of 128 columns took 48 us, so 29), a warp adds up 8 pages x 4 nodes together,
+// and a warp then finds each node's border.
+constexpr int kSelectNodes = 4, kSelectLane = 32;       // keys a lane keeps in registers
+template <typename CT, int D>
+__global__ void __launch_bounds__(kSelectThreads) page_select_nodes_kernel(const __grid_constant__ SelectArgs a) {
+  constexpr int WARPS = kSelectThreads / 32, E = D >= 32 ? D / 32 : 1, BATCH = 8, NB = kSelectNodes;
+  __shared__ double s_q[NB][D];
+  pdl_launch_dependents();
+  const int id = blockIdx.x / a.cluster, rank = blockIdx.x % a.cluster, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int groups = ceil_div(a.T, NB), h = id % a.Hkv, t0 = id / a.Hkv % groups * NB, b = id / a.Hkv / groups;
+  const int full = clamp_int(a.lens[b], 0, a.ppr * kPagePos) / kPagePos, nodes = a.nodes ? clamp_int(a.nodes[b], 0, a.T) : a.T;
+  auto item = [&](int k) { return ((long long)b * a.T + t0 + k) * a.Hkv + h; };
+  // (what decides the next returns is the same for the whole cluster)
+  if (rank == 0) {
+    for (int i = tid; i < NB * a.select; i += kSelectThreads) {
+      const int k = i / a.select, j = i % a.select;
+      if (t0 + k >= a.T) break;
+      if (t0 + k >= nodes || j >= full) a.pages[item(k) * a.select + j] = -1;
+      else if (full <= a.select) a.pages[item(k) * a.select + j] = j;
+    }
+  }
+  if (t0 >= nodes || full <= a.select) return;
+  for (int i = tid; i < NB * D; i += kSelectThreads) {
+    const int k = i / D, d = i % D;
+    double s = 0.;
+    if (t0 + k < nodes) {
+      const CT* src = reinterpret_cast<const CT*>(a.q) + ((long long)b * a.T + t0 + k) * a.q_stride + h * a.G * D + d;
+      for (int g = 0; g < a.G; ++g) s += (double)to_f(src[g * D]);
+    }
+    s_q[k][d] = s;
+  }
+  __syncthreads();
+  {
+    double q[NB][E];
+#pragma unroll
+    for (int k = 0; k < NB; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e) q[k][e] = lane * E + e < D ? s_q[k][lane * E + e] : 0.;
+    const float* m = a.means + ((long long)b * a.ppr * a.Hkv + h) * D + (lane * E < D ? lane * E : 0);
+    const long long step = (long long)a.Hkv * D;
+    for (int p0 = (rank * WARPS + warp) * BATCH; p0 < full; p0 += a.cluster * WARPS * BATCH) {
+      float x[BATCH][E];
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        const float* src = m + min(p0 + k, full - 1) * step;
+        if constexpr (E == 4) *reinterpret_cast<float4*>(x[k]) = *reinterpret_cast<const float4*>(src);
+        else if constexpr (E == 2) *reinterpret_cast<float2*>(x[k]) = *reinterpret_cast<const float2*>(src);
+        else x[k][0] = *src;
+      }
+      double s[BATCH * NB];                                 // sum of page i / NB, node i % NB
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          double v = 0.;
+#pragma unroll
+          for (int e = 0; e < E; ++e) if (lane * E < D) v += q[n][e] * (double)x[k][e];
+          s[k * NB + n] = v;
+        }
+      // 32 sums over 32 lanes: every step halves the sums a lane carries on with, lane i ends with sum i
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) {
+#pragma unroll
+        for (int i = 0; i < o; ++i) {
+          const bool up = lane & o;
+          const double give = up ? s[i] : s[i + o], keep = up ? s[i + o] : s[i];
+          s[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+      }
+      const int p = p0 + lane / NB, n = lane % NB;
+      if (p < full && t0 + n < nodes) a.keys[item(n) * a.ppr + p] = s[0] != s[0] ? 0ull : order_bits64(s[0] + 0.);
+    }
+  }
+  if (a.cluster > 1) {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (rank >= NB) return;
+  } else {
+    __threadfence_block();
+    __syncthreads();
+  }
+  // a warp for a node, in as many CTAs of the cluster as there are
+  const int share = min(a.cluster, NB);
+  for (int k = rank + warp * share; k < NB && t0 + k < nodes; k += WARPS * share) {
+    const unsigned long long* keys = a.keys + item(k) * a.ppr;
+    int* out = a.pages + item(k) * a.select;
+    unsigned long long mine[kSelectLane];
+#pragma unroll
+    for (int i = 0; i < kSelectLane; ++i) mine[i] = lane + i * 32 < full ? __ldcg(keys + lane + i * 32) : 0ull;
+    auto count = [&](unsigned long long x) {                // keys that are at least x (x > 0)
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < kSelectLane; ++i) n += mine[i] >= x;
+#pragma unroll 8
+      for (int p = lane + kSelectLane * 32; p < full; p += 32) n += __ldcg(keys + p) >= x;
+      return __reduce_add_sync(0xffffffffu, n);
+    };
+    unsigned long long border = 0;
+    bool exact = false;
+    for (int bit = 63; bit >= 0 && !exact; --bit) {
+      const unsigned long long candidate = border | (1ull << bit);
+      const int n = count(candidate);
+      if (n >= a.select) border = candidate;
+      exact = n == a.select;
+    }
+    const int room = exact ? full : a.select - (border == ~0ull ? 0 : count(border + 1));
+    const unsigned before = (1u << lane) - 1;
+    int ties = 0, done = 0;
+    auto list = [&](int p, unsigned long long key) {
+      const bool tie = p < full && key == border;
+      unsigned m = __ballot_sync(0xffffffffu, tie);
+      const bool in = p < full && (key > border || (tie && ties + __popc(m & before) < room));
+      ties += __popc(m);
+      m = __ballot_sync(0xffffffffu, in);
+      const int at = done + __popc(m & before);
+      if (in && at < a.select) out[at] = p;
+      done += __popc(m);
+    };
+#pragma unroll
+    for (int i = 0; i < kSelectLane; ++i) {
+      if (i * 32 >= full) break;
+      list(lane + i * 32, mine[i]);
+    }
+    for (int p0 = kSelectLane * 32; p0 < full; p0 += 32) list(p0 + lane, p0 + lane < full ? __ldcg(keys + p0 + lane) : 0ull);
   }
 }
 

@@ -382,8 +382,9 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
 
   clear_dead_rows<CT>(a, D);
   Walk<PAGED> w(a, R);
-  if (!w.begin()) return;
-  if (PAGED) pdl_wait();                                    // the selection
+  const bool work = w.begin();
+  if (PAGED) pdl_wait();                                    // the selection (every CTA: what comes after waits for this launch alone)
+  if (!work) return;
   int lines_of = -1;                                        // sequence whose lines are in shared memory
   int n = 0;                                                // chunks so far
   if (TMA) {

@@ -113,8 +113,9 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
 
   clear_dead_rows<bf16>(a, D);
   Walk<PAGED> w(a, kTcRows);
-  if (!w.begin()) return;                                          // (the same answer in every warp)
-  if (PAGED) pdl_wait();                                           // the selection
+  const bool work = w.begin();                                     // (the same answer in every warp)
+  if (PAGED) pdl_wait();                                           // the selection (every CTA: what comes after waits for this launch alone)
+  if (!work) return;
   if (tid == 0) {
     for (int s = 0; s < KK; ++s) { tc::mbar_init(k_full(s), 1); tc::mbar_init(k_empty(s), 1); }
     for (int s = 0; s < KV; ++s) { tc::mbar_init(v_full(s), 1); tc::mbar_init(v_empty(s), 1); }

@@ -164,6 +164,8 @@ PAGED = [
     ([0], 1, 1, 1, 16, 1, None), ([64], 1, 2, 2, 64, 1, None), ([63], 2, 4, 2, 64, 3, None), ([1000, 130], 3, 8, 2, 128, 4, [3, 2]),
     ([700, 64, 65, 5], 2, 20, 1, 64, 5, [2, 0, 1, 2]), ([2000], 1, 40, 2, 32, 7, None), ([5000], 4, 4, 4, 16, 30, None), ([640], 70, 2, 1, 64, 2, [70]),
     ([2000, 700], 1, 1, 1, 64, 9, None), ([1500], 2, 3, 1, 128, 8, None),
+    # more pages than a thread's or a lane's registers hold keys of
+    ([160003], 1, 2, 1, 16, 9, None), ([70003, 160000], 5, 1, 1, 16, 40, [5, 3]),
 ]
 
 
@@ -276,7 +278,9 @@ def test_cache_weights(bpd, lens, nodes, heads, kv_heads, dim, dtype):
 
 
 EVICT = [(1, [1], 1, 16, 1, 0, "bf16"), (2, [65, 10, 64], 2, 32, 20, 5, "fp32"), (1, [522], 4, 64, 512, 64, "fp32"), (3, [700, 300], 2, 128, 100, 100, "bf16"),
-         (1, [1500, 1], 3, 64, 1, 0, "bf16"), (2, [3000], 2, 16, 2999, 7, "bf16"), (1, [1024, 513, 512], 1, 32, 512, 0, "fp32")]
+         (1, [1500, 1], 3, 64, 1, 0, "bf16"), (2, [3000], 2, 16, 2999, 7, "bf16"), (1, [1024, 513, 512], 1, 32, 512, 0, "fp32"),
+         # more slots than registers hold keys of
+         (1, [9000, 100], 1, 16, 700, 33, "bf16"), (1, [20000, 17001], 1, 16, 9000, 50, "fp32")]
 
 
 @pytest.mark.parametrize("kind", ["random", "ties", "odd"])
@@ -301,6 +305,25 @@ def test_cache_evict(bpd, layers, lens, kv_heads, dim, budget, recent, dtype, ki
     got = bpd.bpd_op_cache_evict(w, p, k, v, table, _dev(c.lens), _dev(seen), budget, recent)
     for x, y in zip((got, w, p, k, v), want):
         assert np.array_equal(x.float().cpu().numpy(), np.asarray(y, np.float32), equal_nan=True)
+
+
+# calls side by side on two streams, each with a scratch and outputs of its own
+def test_two_streams_do_not_meet(bpd):
+    import torch
+    cases = [Case(21, [700, 90, 1500], 6, 4, 2, 64, "bf16"), Case(22, [1200], 40, 4, 1, 128, "bf16"), Case(23, [900, 10], 5, 2, 1, 32, "fp32")]
+    args = [c.drafted() + c.pools(0) + (_dev(c.lens), _dev(c.parents)) for c in cases]
+    alone = [bpd.bpd_op_tree_attention(*a) for a in args]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in args]
+    got = [[] for _ in args]
+    for _ in range(20):
+        for a, s, g in zip(args, streams, got):
+            with torch.cuda.stream(s):
+                g.append(bpd.bpd_op_tree_attention(*a))
+    torch.cuda.synchronize()
+    for want, g in zip(alone, got):
+        assert all(bool((x == want).all()) for x in g)
+    bpd.bpd_op_status()                                      # no wait has expired
 
 
 # a program's step: attention over the cache and the tree, commit, weights, eviction, and the next step's attention over what is
