@@ -18,7 +18,6 @@
 // core's own additions truncate).
 #pragma once
 #include "attention.cuh"
-#include "gemm_tc.cuh"
 #include "cache_index.hpp"
 
 namespace bpd {
@@ -58,39 +57,8 @@ struct AttnArgs {
   int2* info;                                  // per tile: 2 * first CTA that has units of it + the slot of its partial result; last CTA
 };
 
-// ---------------------------------------------------------------- waits and loads
-// A wait of some operator's kernel has expired on this device since it was last asked (see bpd_op_status).
-static __device__ int g_wait_expired;
-
-__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* dead) {
-  if (tc::mbar_try_wait(bar, parity)) return true;
-  const unsigned long long t0 = clock64();
-  for (;;) {
-#pragma unroll 1
-    for (int i = 0; i < 64; ++i)
-      if (tc::mbar_try_wait(bar, parity)) return true;
-    if (*dead) return false;
-    if ((unsigned long long)(clock64() - t0) > tc::kSpinCycles) {
-      *dead = 1;
-      return false;
-    }
-  }
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// A box of a map's only matrix.
-__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst), "l"(map),
-               "r"(bar), "r"(x), "r"(y), "r"(0) : "memory");
-}
-
-// kp, vp: the pools as [n_pages * 64][Hkv * D]; kn, vn: the drafted nodes' rows.
-struct TcMaps { CUtensorMap kp, vp, kn, vn; };
-
-// ---------------------------------------------------------------- layouts
 // Shared-memory layout of a chunk's rows.  bf16: panels of up to 64 columns, their 16-byte pieces XOR-swizzled so that eight
-// consecutive rows' same piece lies in eight different 16-byte columns of the banks (for 64 columns: what TMA's 128-byte
-// swizzle writes); fp32: padded rows (see attention.cuh).
+// consecutive rows' same piece lies in eight different 16-byte columns of the banks; fp32: padded rows (see attention.cuh).
 template <typename CT, int D>
 struct Rows {
   static constexpr bool F32 = sizeof(CT) == 4;
@@ -119,7 +87,7 @@ struct Shape {
   static constexpr int MERGE = WK * R * MP * 4;
   static constexpr int STAGES = F32 ? (D >= 64 ? 2 : 3) : (D >= 128 ? 3 : 4);
   static constexpr int RING = STAGES * Rows<CT, D>::STAGE;
-  static constexpr int SMEM = 1024 + Q_BYTES + (RING > MERGE ? RING : MERGE);   // (TMA's tiles begin at multiples of 1024)
+  static constexpr int SMEM = Q_BYTES + (RING > MERGE ? RING : MERGE);
   static constexpr int CTAS_PER_SM = F32 ? (D >= 128 ? 1 : (WR < 4 ? 3 : 2)) : (D >= 128 ? 2 : 3);
 };
 
@@ -359,23 +327,21 @@ __device__ __forceinline__ void clear_dead_rows(const AttnArgs& a, int D) {
   }
 }
 
-// TMA: pages come as TMA tiles (bf16, heads of 64 and 128), else by 16-byte asynchronous copies of every thread.  With the
-// copies, half of the loop's instructions were addresses; TMA's tensor maps cost the host a few microseconds a call, so small
-// calls do without.
-template <typename CT, int D, int WR, bool PAGED, bool TMA>
-__global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tree_attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ TcMaps maps) {
+// (With the pages of bf16 caches brought by TMA instead of every thread's 16-byte copies, the times were the same to 2 %, and
+// the tensor maps cost the host a microsecond a call.)
+template <typename CT, int D, int WR, bool PAGED>
+__global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tree_attention_kernel(const __grid_constant__ AttnArgs a) {
   using S = Shape<CT, D, WR>;
   using L = Rows<CT, D>;
   pdl_launch_dependents();
   constexpr bool F32 = S::F32;
   constexpr int R = S::R, WK = S::WK, KW = S::KW, KT = D / 16, NT = KW / 8, DT = D / 8;
   extern __shared__ __align__(128) uint8_t ta_smem[];
-  __shared__ __align__(8) unsigned long long s_full[S::STAGES];
-  __shared__ int s_dead, s_keys[S::STAGES], s_pages[kPagesAhead];
+  __shared__ int s_keys[S::STAGES], s_pages[kPagesAhead];
   __shared__ Lines s_lines;
   __shared__ float s_m[WK][R], s_l[WK][R];
-  uint8_t* ring = ta_smem + ((1024u - (s_addr(ta_smem) & 1023u)) & 1023u);
-  bf16* qs = reinterpret_cast<bf16*>(ring + (S::SMEM - 1024 - S::Q_BYTES));
+  bf16* qs = reinterpret_cast<bf16*>(ta_smem);
+  uint8_t* ring = ta_smem + S::Q_BYTES;
   const uint32_t ring_s = s_addr(ring);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
   const int wr = warp % WR, wk = warp / WR;
@@ -387,15 +353,6 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
   if (!work) return;
   int lines_of = -1;                                        // sequence whose lines are in shared memory
   int n = 0;                                                // chunks so far
-  if (TMA) {
-    if (tid == 0) {
-      for (int s = 0; s < S::STAGES; ++s) tc::mbar_init(s_addr(&s_full[s]), 1);
-      s_dead = 0;
-      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    __syncthreads();
-  }
-
   do {
     const int rows = w.rows(), b = w.b, cache_chunks = w.cache_chunks(), c_begin = w.c_begin, c_end = w.c_end;
     auto node_of = [&](int r) { return w.node_of(r); };
@@ -412,20 +369,6 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
       const uint32_t ks = ring_s + stage * L::STAGE, vs = ks + L::K_BYTES;
       const bool node = c >= cache_chunks;
       if (tid == 0) s_keys[stage] = n_keys;                 // (read behind the barrier at the chunk's turn)
-      if constexpr (TMA) {
-        if (tid == 0) {
-          // (a page that is not there: some page comes instead, all of it masked)
-          const int y = node ? b * a.T + (c - cache_chunks) * kChunk : max(page, 0) * kPagePos;
-          const uint32_t bar = s_addr(&s_full[stage]);
-          tc::mbar_expect_tx(bar, L::STAGE);
-#pragma unroll
-          for (int p = 0; p < D / 64; ++p) {
-            load_box(ks + p * kChunk * 128, node ? &maps.kn : &maps.kp, bar, tl.h * D + p * 64, y);
-            load_box(vs + p * kChunk * 128, node ? &maps.vn : &maps.vp, bar, tl.h * D + p * 64, y);
-          }
-        }
-        return;
-      }
       const long long at = node ? ((long long)b * a.T + (c - cache_chunks) * kChunk) * a.kv_stride + tl.h * D : ((long long)max(page, 0) * kPagePos * a.Hkv + tl.h) * D;
       const long long step = node ? a.kv_stride : (long long)a.Hkv * D;
       constexpr int PER_PASS = kThreads / L::PIECES;
@@ -487,7 +430,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
 #pragma unroll
     for (int s = 0; s < S::STAGES - 1; ++s) {
       if (c_begin + s < c_end) load(c_begin + s, (n + s) % S::STAGES);
-      if (!TMA) asm volatile("cp.async.commit_group;" ::: "memory");
+      asm volatile("cp.async.commit_group;" ::: "memory");
     }
     // the nodes' lines, where the run reaches the tree (the loop's barrier follows; those of the sequence before have been used)
     if (c_end > cache_chunks && lines_of != b) {
@@ -496,30 +439,20 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
     }
     for (int c = c_begin; c < c_end; ++c, ++n) {
       const int stage = n % S::STAGES;
-      if (!TMA) asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 2) : "memory");
-      __syncthreads();                                      // the stage before has been used (and, copied, the chunk is there)
+      asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 2) : "memory");
+      __syncthreads();                                      // the chunk is there, and the stage before it has been used
       {
         const int cn = c + S::STAGES - 1;
         if (cn < c_end) {
           if ((cn - c_begin) % kPagesAhead == 0) look_up(cn);
           load(cn, (n + S::STAGES - 1) % S::STAGES);
         }
-        if (!TMA) asm volatile("cp.async.commit_group;" ::: "memory");
+        asm volatile("cp.async.commit_group;" ::: "memory");
       }
       const uint8_t* kb = ring + stage * L::STAGE;
       const uint8_t* vb = kb + L::K_BYTES;
       const uint32_t ks = ring_s + stage * L::STAGE, vs = ks + L::K_BYTES;
       const int n_keys = s_keys[stage], key0 = wk * KW;
-      if constexpr (TMA) {
-        // (after an expired wait the rest runs on whatever is there: see bpd_op_status)
-        wait_bar(s_addr(&s_full[stage]), (n / S::STAGES) & 1, &s_dead);
-        if (n_keys < kChunk) {
-          for (int i = n_keys * L::PIECES + tid; i < kChunk * L::PIECES; i += kThreads)
-            *reinterpret_cast<uint4*>(const_cast<uint8_t*>(vb) + L::v_at(i / L::PIECES, i % L::PIECES)) = make_uint4(0u, 0u, 0u, 0u);
-          fence_async_shared();
-          __syncthreads();
-        }
-      }
 
       // scores of the warp's 16 rows and KW keys
       float s[NT][4];
@@ -722,7 +655,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
     }
 
     // join the warps that shared the rows
-    if (!TMA) asm volatile("cp.async.wait_all;" ::: "memory");
+    asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();                                        // the ring has been used
     l0 += __shfl_xor_sync(0xffffffffu, l0, 1); l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
     l1 += __shfl_xor_sync(0xffffffffu, l1, 1); l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
@@ -766,11 +699,9 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
       }
     }
     if (!a.split) return;
-    if (TMA) fence_async_shared();                          // the ring's next contents come by TMA
     if (c_begin == 0 && tid == 0) a.info[tl.id] = make_int2(blockIdx.x * 2 + w.slot, w.last_cta);
     __syncthreads();                                        // the ring, the lines and the sums are free again
   } while (w.next());
-  if (TMA && tid == 0 && s_dead) g_wait_expired = 1;
 }
 
 // Joins the partial results of the tiles that more than one CTA worked on.  grid: (tiles that could be, rows / (4 / SHARE)):

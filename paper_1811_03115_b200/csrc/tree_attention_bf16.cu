@@ -11,7 +11,11 @@ namespace tree {
 
 // Calls whose work is cut into runs, heads of 64 and 128: with more than 32 rows to a key head the tiles are 128 rows and go
 // to the 5th-generation tensor cores.  With fewer, a tile's products are short and its softmax is one warp's, and the kernel
-// whose four warps share the keys is the faster one.  SWEEP
+// whose four warps share the keys is the faster one.  us of that kernel / of the 128-row one, 8 key heads, before either had its
+// present form:
+//   rows                                 8        16        32        48        64       128
+//   8 x 8000 positions, heads of 128  55 / 59   59 / 63   68 / 66   98 / 71  103 / 75  184 / 102
+//   8 x 8000 positions, heads of 64   36 / 46   37 / 46   46 / 50   84 / 54   87 / 56  153 / 78
 template <int D, bool PAGED>
 int plan_tc(const AttnArgs& a, AttnPlan* p) {
   const long long per_head = PAGED ? ceil_div(a.G, kTcRows) : ceil_div(a.T * a.G, kTcRows);
@@ -42,9 +46,12 @@ int maps_of(const AttnArgs& a, TcMaps* maps) {
 }
 
 template <int D, bool PAGED>
-int launch_tc(const AttnArgs& a, const TcMaps& maps, const AttnPlan& p, cudaStream_t st) {
+int launch_tc(const AttnArgs& a, const AttnPlan& p, cudaStream_t st) {
   using S = TcShape<D>;
-  int rc = ensure_smem_limit(reinterpret_cast<const void*>(tree_attention_tc_kernel<D, PAGED>), S::SMEM);
+  TcMaps maps;
+  int rc = maps_of<D>(a, &maps);
+  if (rc) return rc;
+  rc = ensure_smem_limit(reinterpret_cast<const void*>(tree_attention_tc_kernel<D, PAGED>), S::SMEM);
   if (rc) return rc;
   BPD_CUDA(launch_k(tree_attention_tc_kernel<D, PAGED>, dim3(p.ctas), dim3(kTcThreads), S::SMEM, st, PAGED, a, maps));
   ++g_launches;
@@ -61,21 +68,11 @@ template <> int plan_attention<bf16>(const AttnArgs& a, bool paged, int D, AttnP
   })
 }
 template <> int launch_attention<bf16>(const AttnArgs& a, bool paged, int D, const AttnPlan& plan, cudaStream_t st) {
-  TcMaps maps;
   BPD_TREE_BY_DIM({
     if constexpr (DD >= 64) {
-      if (plan.split) {
-        const int rc = maps_of<DD>(a, &maps);
-        if (rc) return rc;
-        if (plan.tc) return paged ? launch_tc<DD, true>(a, maps, plan, st) : launch_tc<DD, false>(a, maps, plan, st);
-        return by_rows<bf16, DD>(a, paged, [&](auto wr, auto pg) {
-          if constexpr (decltype(wr)::value <= 2) return launch_one<bf16, DD, decltype(wr)::value, decltype(pg)::value, true>(a, maps, plan, st);
-          else return fail(BPD_E_UNSUPPORTED, "no kernel for %d rows", a.T * a.G);   // (more than 32 rows: plan.tc)
-        });
-      }
+      if (plan.tc) return paged ? launch_tc<DD, true>(a, plan, st) : launch_tc<DD, false>(a, plan, st);
     }
-    memset(&maps, 0, sizeof(maps));
-    return by_rows<bf16, DD>(a, paged, [&](auto wr, auto pg) { return launch_one<bf16, DD, decltype(wr)::value, decltype(pg)::value, false>(a, maps, plan, st); });
+    return by_rows<bf16, DD>(a, paged, [&](auto wr, auto pg) { return launch_one<bf16, DD, decltype(wr)::value, decltype(pg)::value>(a, plan, st); });
   })
 }
 

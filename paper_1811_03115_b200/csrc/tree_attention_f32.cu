@@ -11,9 +11,7 @@ template <> int plan_attention<float>(const AttnArgs& a, bool paged, int D, Attn
   BPD_TREE_BY_DIM(return by_rows<float, DD>(a, paged, [&](auto wr, auto pg) { return plan_one<float, DD, decltype(wr)::value, decltype(pg)::value>(a, plan); });)
 }
 template <> int launch_attention<float>(const AttnArgs& a, bool paged, int D, const AttnPlan& plan, cudaStream_t st) {
-  TcMaps maps;                                 // (none)
-  memset(&maps, 0, sizeof(maps));
-  BPD_TREE_BY_DIM(return by_rows<float, DD>(a, paged, [&](auto wr, auto pg) { return launch_one<float, DD, decltype(wr)::value, decltype(pg)::value, false>(a, maps, plan, st); });)
+  BPD_TREE_BY_DIM(return by_rows<float, DD>(a, paged, [&](auto wr, auto pg) { return launch_one<float, DD, decltype(wr)::value, decltype(pg)::value>(a, plan, st); });)
 }
 
 }  // namespace tree

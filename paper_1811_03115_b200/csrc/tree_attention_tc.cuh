@@ -15,6 +15,7 @@
 // Every wait is bounded; on expiry the CTA notes it (see bpd_op_status), waits (bounded) for its copies and products in
 // flight, frees its tensor memory and returns.
 #pragma once
+#include "gemm_tc.cuh"
 #include "tree_attention.cuh"
 
 namespace bpd {
@@ -24,10 +25,11 @@ constexpr int kTcThreads = 192, kTcRows = 128;
 
 template <int D>
 struct TcShape {
-  // Stages of keys and of values.  A chunk's keys are used up as soon as its scores are there, a chunk ahead of their softmax;
-  // its values two softmaxes later.  So most of the room goes to the values (with two stages each and one order of issue,
-  // loads had one softmax of time, and a third of every chunk's 3400 cycles was spent waiting for them).
-  static constexpr int KK = D == 128 ? 1 : 2, KV = D == 128 ? 3 : 4;
+  // Stages of keys and of values, filled independently: a chunk's keys are used up as soon as its scores are there, a chunk
+  // ahead of their softmax; its values two softmaxes later.  (In one order of issue, keys waited behind values for whose place a
+  // product had to end, and a third of every chunk's 3400 cycles went by waiting.  One stage of keys to three of values: 87 us
+  // instead of 84 for 8 sequences of up to 16000, 128 rows, heads of 128.)
+  static constexpr int KK = 2, KV = D == 128 ? 2 : 4;
   static constexpr int PANELS = D / 64;                       // of 64 columns
   static constexpr int PANEL = kChunk * 128;                  // bytes of a panel of keys or values
   static constexpr int Q_PANEL = kTcRows * 128;
@@ -36,6 +38,34 @@ struct TcShape {
   static constexpr int TMEM_COLS = 256;                       // scores / weights of two chunks (64 columns each), outputs (D)
   static constexpr int CTAS_PER_SM = 2;
 };
+
+// A wait of some operator's kernel has expired on this device since it was last asked (see bpd_op_status).
+static __device__ int g_wait_expired;
+
+__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* dead) {
+  if (tc::mbar_try_wait(bar, parity)) return true;
+  const unsigned long long t0 = clock64();
+  for (;;) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (tc::mbar_try_wait(bar, parity)) return true;
+    if (*dead) return false;
+    if ((unsigned long long)(clock64() - t0) > tc::kSpinCycles) {
+      *dead = 1;
+      return false;
+    }
+  }
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// A box of a map's only matrix.
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst), "l"(map),
+               "r"(bar), "r"(x), "r"(y), "r"(0) : "memory");
+}
+
+// kp, vp: the pools as [n_pages * 64][Hkv * D]; kn, vn: the drafted nodes' rows.
+struct TcMaps { CUtensorMap kp, vp, kn, vn; };
 
 // The same answer in every lane.
 __device__ __forceinline__ bool wait_bar_warp(uint32_t bar, uint32_t parity, volatile int* dead) { return __all_sync(0xffffffffu, wait_bar(bar, parity, dead)); }

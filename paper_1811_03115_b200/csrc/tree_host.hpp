@@ -13,7 +13,10 @@ struct AttnPlan {
   int ctas, tile_rows, tiles, combine_rows, split, tc, end_units;   // tiles: that could be
   size_t part_bytes, info_bytes;
 };
-constexpr int kWholeTileChunks = 6;           // tiles of at most so many chunks get a CTA each
+// Tiles of at most so many chunks get a CTA each and need no join: a second launch and its trips to memory cost as much as
+// five chunks (one token over 57 positions 9.0 us with runs, 6.2 with whole tiles; 512 tiles of up to three chunks 19.9 / 14.4;
+// 16 tiles of up to 135 chunks 19 / 98).
+constexpr int kWholeTileChunks = 6;
 // Rows of a tile: as few as hold all rows of a key head, 64 at most.
 inline int tile_rows_of(bool paged, int rows) { return paged || rows <= 16 ? 16 : (rows <= 32 ? 32 : 64); }
 
@@ -64,13 +67,13 @@ int launch_combine(const AttnArgs& a, const AttnPlan& p, cudaStream_t st) {
   return BPD_OK;
 }
 
-template <typename CT, int D, int WR, bool PAGED, bool TMA>
-int launch_one(const AttnArgs& a, const TcMaps& maps, const AttnPlan& p, cudaStream_t st) {
+template <typename CT, int D, int WR, bool PAGED>
+int launch_one(const AttnArgs& a, const AttnPlan& p, cudaStream_t st) {
   using S = Shape<CT, D, WR>;
-  const auto kernel = tree_attention_kernel<CT, D, WR, PAGED, TMA>;
+  const auto kernel = tree_attention_kernel<CT, D, WR, PAGED>;
   int rc = ensure_smem_limit(reinterpret_cast<const void*>(kernel), S::SMEM);
   if (rc) return rc;
-  BPD_CUDA(launch_k(kernel, dim3(p.ctas), dim3(kThreads), S::SMEM, st, PAGED, a, maps));
+  BPD_CUDA(launch_k(kernel, dim3(p.ctas), dim3(kThreads), S::SMEM, st, PAGED, a));
   ++g_launches;
   return p.split ? launch_combine<CT, D, PAGED>(a, p, st) : BPD_OK;
 }
