@@ -9,13 +9,18 @@
 namespace bpd {
 namespace tree {
 
-// Calls whose work is cut into runs, heads of 64 and 128: with more than 32 rows to a key head the tiles are 128 rows and go
-// to the 5th-generation tensor cores.  With fewer, a tile's products are short and its softmax is one warp's, and the kernel
-// whose four warps share the keys is the faster one.  us of that kernel / of the 128-row one, 8 key heads, before either had its
-// present form:
-//   rows                                 8        16        32        48        64       128
-//   8 x 8000 positions, heads of 128  55 / 59   59 / 63   68 / 66   98 / 71  103 / 75  184 / 102
-//   8 x 8000 positions, heads of 64   36 / 46   37 / 46   46 / 50   84 / 54   87 / 56  153 / 78
+// Calls whose work is cut into runs, heads of 64 and 128: with more than 64 rows to a key head, and with more than 32 where a
+// sequence may have 64 pages or more, tiles are 128 rows and go to the 5th-generation tensor cores.  With fewer, a tile's
+// products are short and its softmax is one warp's or two's; with short sequences, the tile's start and end weigh more than its
+// chunks.  us of the kernel whose four warps share the keys / of the 128-row one, 8 key heads (16 in the last line):
+//   rows                                        16         32         48         64        128
+//   8 sequences of 8000, heads of 128        54 / 68    63 / 68    93 / 70    92 / 68   174 / 79
+//   8 sequences of 8000, heads of 64         35 / 43    40 / 45    56 / 46    57 / 46   103 / 57
+//   1 sequence of 8000, heads of 128         17 / 24    20 / 23    25 / 26    26 / 25    37 / 30
+//   32 sequences of 500, heads of 128        25 / 44    33 / 44    46 / 52    50 / 50    91 / 61
+//   32 sequences of 500, heads of 64         27 / 53    36 / 56    51 / 60    56 / 62   100 / 78
+inline bool many_rows(int rows, long long chunks) { return rows > 64 || (rows > 32 && chunks >= 64); }
+
 template <int D, bool PAGED>
 int plan_tc(const AttnArgs& a, AttnPlan* p) {
   const long long per_head = PAGED ? ceil_div(a.G, kTcRows) : ceil_div(a.T * a.G, kTcRows);
@@ -62,7 +67,7 @@ template <> int plan_attention<bf16>(const AttnArgs& a, bool paged, int D, AttnP
   BPD_TREE_BY_DIM({
     int rc = by_rows<bf16, DD>(a, paged, [&](auto wr, auto pg) { return plan_one<bf16, DD, decltype(wr)::value, decltype(pg)::value>(a, plan); });
     if constexpr (DD >= 64) {
-      if (!rc && plan->split && (paged ? a.G : a.T * a.G) > 32) rc = paged ? plan_tc<DD, true>(a, plan) : plan_tc<DD, false>(a, plan);
+      if (!rc && plan->split && many_rows(paged ? a.G : a.T * a.G, paged ? max_chunks<true>(a) : max_chunks<false>(a))) rc = paged ? plan_tc<DD, true>(a, plan) : plan_tc<DD, false>(a, plan);
     }
     return rc;
   })

@@ -1,5 +1,5 @@
-// The tree attention of tree_attention.cuh on the 5th-generation tensor cores: bf16 caches with heads of 64 or 128, in calls
-// whose work is cut into runs of chunks.
+// The tree attention of tree_attention.cuh on the 5th-generation tensor cores: bf16 caches with heads of 64 or 128, many rows
+// (see many_rows), in calls whose work is cut into runs of chunks.
 //
 // A tile is 128 query rows of a key head (fewer use fewer of the lanes).  Per chunk of 64 keys: S = Q K^T (tcgen05.mma, both
 // operands in shared memory) into tensor memory; a thread per row takes its 64 scores, and puts the weights back where the
@@ -14,6 +14,11 @@
 //
 // Every wait is bounded; on expiry the CTA notes it (see bpd_op_status), waits (bounded) for its copies and products in
 // flight, frees its tensor memory and returns.
+//
+// What bounds it: 8 sequences of 8000 and 128 rows, heads of 128, move 268 MB in 70 us of the launch's 79 with the join -- 0.58
+// of the copy's rate; the tensor pipe is active 39 % of the time.  A chunk takes a CTA 3000 cycles: about 1000 exponentials and
+// the weights' planes, 240 the maximum, up to 1200 waiting for keys or values, the rest tensor-memory traffic and barriers.  Heads of
+// 64: 2100 cycles, half of them exponentials.
 #pragma once
 #include "gemm_tc.cuh"
 #include "tree_attention.cuh"
@@ -216,8 +221,11 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
     if (lane == 0) {
       const uint32_t id_s = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kChunk >> 3) << 17) | ((uint32_t)(kTcRows >> 4) << 24);
       const uint32_t id_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTcRows >> 4) << 24);
-      auto scores = [&](int n) {
+      auto scores = [&](int n, bool first) {
         if (!wait_bar(k_full(n), (n / KK) & 1, dead)) return false;
+        // The scores take the place of the weights of two chunks before, whose product must have read them: products are in
+        // order only where they add to the same sums.  (A tile's first chunk comes when all products before it are done.)
+        if (!first && n >= 2 && !wait_bar(pv_done, (n - 2) & 1, dead)) return false;
         tc::tc_fence_after();
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
@@ -233,10 +241,10 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
         ok = wait_bar(q_ready, tile & 1, dead);
         tc::tc_fence_after();
         const int count = w.c_end - w.c_begin;
-        if (ok) ok = scores(n);
+        if (ok) ok = scores(n, true);
         for (int i = 0; i < count && ok; ++i, ++n) {
-          // (the next chunk's scores take the place of weights whose product was issued before them)
-          if (i + 1 < count && !(ok = scores(n + 1))) break;
+          // (the next chunk's scores run ahead, under this one's softmax)
+          if (i + 1 < count && !(ok = scores(n + 1, false))) break;
           if (!(ok = wait_bar(p_ready(n & 1), (n >> 1) & 1, dead)) || !(ok = wait_bar(v_full(n), (n / KV) & 1, dead))) break;
           tc::tc_fence_after();
 #pragma unroll
@@ -400,6 +408,8 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
       }
       if (!ok) break;
       // ---- the tile's result
+      // (a wait by parity tells a phase from the one before it, not from the one two before: a softmax may be two products ahead)
+      if (count > 1 && !(ok = wait_bar_warp(pv_done, (n - 2) & 1, dead))) break;
       if (!(ok = wait_bar_warp(pv_done, (n - 1) & 1, dead))) break;
       tc::tc_fence_after();
       if (tree && !(ok = meet())) break;
@@ -444,7 +454,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
           if (!whole) {
             // 32 rows x 32 columns through the warp's own rows of the queries' place, so that stores are whole lines
             uint8_t* mine = gen + warp * 4096;
-            __syncwarp();
+            __syncwarp();                                          // (what was there has been read)
 #pragma unroll
             for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(mine + lane * 128 + (((e / 4) ^ (lane & 7)) * 16)) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
             __syncwarp();
@@ -454,6 +464,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
               const uint4 y = *reinterpret_cast<const uint4*>(mine + row * 128 + ((piece ^ (row & 7)) * 16));
               if (warp * 32 + row < rows) *reinterpret_cast<uint4*>(part + (long long)(warp * 32 + row) * D + d + piece * 4) = y;
             }
+            __syncwarp();                                          // (the next tile's queries go there)
           }
         }
         if (r < rows) {

@@ -98,6 +98,7 @@ TREES = [
     ([129], 200, 2, 1, 64, "random", None), ([20], 256, 1, 1, 32, "chain", None), ([64], 100, 2, 2, 128, "star", None),
     ([2500, 1, 640, 64], 3, 16, 1, 128, "random", [3, 1, 2, 3]), ([40] * 130, 2, 2, 1, 16, "chain", None),
     ([1500], 1, 1, 1, 64, "chain", None), ([1500, 30], 3, 1, 1, 128, "chain", None), ([900], 5, 3, 1, 16, "random", None), ([2000, 1], 70, 4, 2, 128, "random", [70, 9]),
+    ([4100, 300], 20, 4, 2, 64, "random", [20, 7]), ([4160, 0], 13, 3, 1, 128, "chain", [13, 2]), ([600, 448, 1], 256, 2, 2, 64, "random", [256, 130, 3]),
 ]
 
 
@@ -129,7 +130,7 @@ def test_tree_attention_of_slices_of_one_projection(bpd, dtype):
 
 # siblings hold infinities and NaN: only their own lines may see them
 @pytest.mark.parametrize("dtype,dim,nodes,length", [("bf16", 64, 9, 10), ("fp32", 64, 9, 10), ("bf16", 128, 40, 0), ("fp32", 16, 20, 10), ("bf16", 64, 9, 500),
-                                                    ("bf16", 128, 70, 1000), ("fp32", 32, 70, 600)])
+                                                    ("bf16", 128, 70, 1000), ("bf16", 64, 100, 700), ("fp32", 32, 70, 600)])
 def test_values_that_are_no_numbers_stay_in_their_line(bpd, dtype, dim, nodes, length):
     c = Case(5, [length, 0], nodes, 2, 1, dim, dtype, tree="star")
     c.parents[:, 3] = 1
@@ -153,6 +154,10 @@ def test_values_of_device_arrays_are_not_trusted(bpd, dtype):
     c.parents[0] = [5, 1, 7, -3, 2, 2]
     out, lse = bpd.bpd_op_tree_attention(*c.drafted(), *c.pools(0), _dev(c.lens), _dev(c.parents), want_lse=True)
     c.check(out, *plain.attention(c.q, c.k_new[0], c.v_new[0], c.k[0], c.v[0], c.table, c.lens, c.parents, c.nodes, c.scale), lse)
+    many = Case(7, [500, 450, 700], 40, 4, 2, 64, dtype, spare=2)
+    many.table[0, 2], many.table[1, 7], many.table[2, 0] = -7, len(many.k[0]), 2 ** 31 - 1
+    out, lse = bpd.bpd_op_tree_attention(*many.drafted(), *many.pools(0), _dev(many.lens), _dev(many.parents), want_lse=True)
+    many.check(out, *plain.attention(many.q, many.k_new[0], many.v_new[0], many.k[0], many.v[0], many.table, many.lens, many.parents, many.nodes, many.scale), lse)
     lens, nodes = np.array([-5, 2 ** 31 - 1, 90], np.int32), np.array([99, -2, 2 ** 31 - 1], np.int32)
     c.k[:], c.v[:] = np.nan_to_num(c.k), np.nan_to_num(c.v)
     out, lse = bpd.bpd_op_tree_attention(*c.drafted(), *c.pools(0), _dev(lens), _dev(c.parents), _dev(nodes), want_lse=True)
@@ -165,6 +170,7 @@ PAGED = [
     ([700, 64, 65, 5], 2, 20, 1, 64, 5, [2, 0, 1, 2]), ([2000], 1, 40, 2, 32, 7, None), ([5000], 4, 4, 4, 16, 30, None), ([640], 70, 2, 1, 64, 2, [70]),
     ([2000, 700], 1, 1, 1, 64, 9, None), ([1500], 2, 3, 1, 128, 8, None),
     # more pages than a thread's or a lane's registers hold keys of
+    ([1500, 90], 2, 80, 1, 64, 9, None), ([5000], 1, 40, 1, 128, 70, None), ([900, 64], 70, 66, 1, 64, 8, [70, 3]),
     ([160003], 1, 2, 1, 16, 9, None), ([70003, 160000], 5, 1, 1, 16, 40, [5, 3]),
 ]
 
@@ -305,6 +311,33 @@ def test_cache_evict(bpd, layers, lens, kv_heads, dim, budget, recent, dtype, ki
     got = bpd.bpd_op_cache_evict(w, p, k, v, table, _dev(c.lens), _dev(seen), budget, recent)
     for x, y in zip((got, w, p, k, v), want):
         assert np.array_equal(x.float().cpu().numpy(), np.asarray(y, np.float32), equal_nan=True)
+
+
+# what a race would show: the same call fifty times, with other work on the device between; many short runs that end and begin
+# inside tiles, and long ones
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens,nodes,heads,kv_heads,dim,select", [([900], 70, 66, 1, 64, 8), ([900], 60, 80, 1, 128, 9), ([3000, 100, 2000], 40, 4, 1, 128, 0),
+                                                                  ([2500] * 5, 64, 4, 2, 64, 0), ([5000], 5, 8, 2, 64, 20), ([700] * 20, 16, 2, 2, 32, 0)])
+def test_the_same_call_gives_the_same_bits(bpd, lens, nodes, heads, kv_heads, dim, select, dtype):
+    import torch
+    c = Case(31, lens, nodes, heads, kv_heads, dim, dtype)
+    q, k_new, v_new = c.drafted()
+    k, v, table = c.pools(0)
+    lens_d, parents = _dev(c.lens), _dev(c.parents)
+    means = torch.zeros((1,) + c.table.shape + (kv_heads, dim), device="cuda")
+    bpd.bpd_op_page_means(k[None], table, torch.zeros_like(lens_d), lens_d, means)
+
+    def call():
+        if select:
+            return bpd.bpd_op_page_attention(q, k_new, v_new, k, v, table, means[0], lens_d, parents, select)
+        return bpd.bpd_op_tree_attention(q, k_new, v_new, k, v, table, lens_d, parents)
+    first, noise = call(), torch.empty(1 << 22, device="cuda")
+    same = []
+    for i in range(50):
+        if i % 3 == 0:
+            noise.normal_()
+        same.append((call() == first).all())
+    assert bool(torch.stack(same).all())
 
 
 # calls side by side on two streams, each with a scratch and outputs of its own
