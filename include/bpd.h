@@ -322,7 +322,10 @@ int bpd_op_linear(const void* x, const void* w, const void* bias, int rows, int 
  * parent that does not lie before its node is taken as -1, and a page outside
  * [0, n_pages) is no page: its positions count as masked and are not written.
  * Two table entries of different rows may name the same page as long as no call
- * writes a position of it.  capacity = pages_per_row * 64. */
+ * writes a position of it.  capacity = pages_per_row * 64.  Limits (BPD_E_SHAPE
+ * beyond them): kv_heads <= 1024, heads <= 4096, batch and layers <= 65535,
+ * n_pages <= 2^24, pages_per_row <= 2^20; other head widths are
+ * BPD_E_UNSUPPORTED.  A refused call leaves everything as it was. */
 typedef struct {
   void* k_pool;               /* device [layers][n_pages][64][kv_heads][head_dim] of dtype, 16-byte aligned */
   void* v_pool;               /* the same for the values; may be NULL where a call only reads keys      */
