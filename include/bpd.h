@@ -368,9 +368,11 @@ int bpd_op_tree_attention(const bpd_cache* cache, const void* q, const void* k_n
  * to positions lens[b], lens[b] + 1, ... of every layer.
  * k_new, v_new: device [layers][batch][nodes] rows, kv_stride elements apart.
  * tokens, top1, parents: device [batch][nodes].  Outputs, device int32:
- * out_lens [batch] (not the array lens), out_accepted [batch], out_path
- * [batch][nodes] (the nodes taken, -1 behind them), out_next [batch]: the
- * prediction after the last node taken, i.e. the next step's last_top1. */
+ * out_lens [batch], out_accepted [batch], out_path [batch][nodes] (the nodes
+ * taken, -1 behind them), out_next [batch]: the prediction after the last node
+ * taken, i.e. what the next step passes as last_top1 (keep two arrays and swap
+ * them).  No output may overlap an input: every CTA of a sequence walks its tree
+ * (BPD_E_INVALID). */
 int bpd_op_tree_commit(const bpd_cache* cache, const void* k_new, const void* v_new, int nodes, int64_t kv_stride,
                        const int32_t* lens, const int32_t* parents, const int32_t* tokens, const int32_t* top1,
                        const int32_t* last_top1, const int32_t* n_nodes, int32_t eos_id, int32_t* out_lens,
@@ -398,7 +400,8 @@ int bpd_op_cache_weights(const bpd_cache* cache, const void* q, int nodes, int h
  * it was.  Slots are then in no order, which attention does not mind and
  * `positions` records.  1 <= budget, 0 <= recent <= budget.
  * weights, positions: device [layers][batch][kv_heads][capacity].  out_lens:
- * device [batch] (not the array lens): min(lens, budget). */
+ * device [batch]: min(lens, budget); may not overlap lens, seen or the page
+ * table (BPD_E_INVALID). */
 size_t bpd_op_cache_evict_scratch_bytes(const bpd_cache* cache, int budget);
 int bpd_op_cache_evict(const bpd_cache* cache, const int32_t* lens, const int32_t* seen, int budget, int recent,
                        float* weights, int32_t* positions, void* scratch, size_t scratch_bytes, int32_t* out_lens,

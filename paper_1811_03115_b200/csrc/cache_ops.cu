@@ -2,6 +2,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "cache_ops.cuh"
 #include "tree_host.hpp"
@@ -106,6 +107,16 @@ int check_scratch(const void* scratch, size_t have, size_t need) {
   if (need == 0) return BPD_OK;
   if (!scratch || !aligned(scratch, 256)) return fail(BPD_E_INVALID, "scratch is null or misaligned");
   if (have < need) return fail(BPD_E_NOMEM, "scratch too small: %zu bytes, %zu needed", have, need);
+  return BPD_OK;
+}
+
+// Outputs that the first CTA of a sequence writes, and arrays that its other CTAs may still have to read, share no memory.
+struct Span { const void* at; size_t bytes; const char* name; };
+int check_apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  for (const Span& o : outs)
+    for (const Span& i : ins)
+      if (o.at && i.at && (uintptr_t)o.at < (uintptr_t)i.at + i.bytes && (uintptr_t)i.at < (uintptr_t)o.at + o.bytes)
+        return fail(BPD_E_INVALID, "%s must not overlap %s, which every CTA of a sequence reads", o.name, i.name);
   return BPD_OK;
 }
 
@@ -224,9 +235,13 @@ int bpd_op_tree_commit(const bpd_cache* cache, const void* k_new, const void* v_
   if (rc || (rc = check_nodes(nodes))) return rc;
   if (!lens || !parents || !tokens || !top1 || !last_top1 || !out_lens || !out_accepted || !out_path || !out_next)
     return fail(BPD_E_INVALID, "null argument");
-  if (out_lens == lens) return fail(BPD_E_INVALID, "out_lens must not be lens: every CTA of a sequence reads its length");
   const long long width = (long long)cache->kv_heads * cache->head_dim;
   if ((rc = check_rows(cache, k_new, kv_stride, width, "k_new")) || (rc = check_rows(cache, v_new, kv_stride, width, "v_new"))) return rc;
+  const size_t per_row = (size_t)cache->batch * 4, per_node = per_row * nodes;
+  if ((rc = check_apart({{out_lens, per_row, "out_lens"}, {out_accepted, per_row, "out_accepted"}, {out_path, per_node, "out_path"}, {out_next, per_row, "out_next"}},
+                        {{lens, per_row, "lens"}, {parents, per_node, "parents"}, {tokens, per_node, "tokens"}, {top1, per_node, "top1"},
+                         {last_top1, per_row, "last_top1"}, {n_nodes, per_row, "n_nodes"}, {cache->page_table, per_row * cache->pages_per_row, "the page table"}})))
+    return rc;
   CommitArgs a;
   a.k_new = k_new; a.v_new = v_new; a.k_pool = cache->k_pool; a.v_pool = cache->v_pool; a.table = cache->page_table; a.lens = lens;
   a.parents = parents; a.tokens = tokens; a.top1 = top1; a.last_top1 = last_top1; a.nodes = n_nodes;
@@ -269,11 +284,13 @@ int bpd_op_cache_evict(const bpd_cache* cache, const int32_t* lens, const int32_
   int rc = check_cache(cache, true);
   if (rc) return rc;
   if (!lens || !seen || !weights || !positions || !out_lens) return fail(BPD_E_INVALID, "null argument");
-  if (out_lens == lens) return fail(BPD_E_INVALID, "out_lens must not be lens: every CTA of a sequence reads its length");
   if (budget < 1) return fail(BPD_E_SHAPE, "budget %d must be at least 1", budget);
   if (recent < 0 || recent > budget) return fail(BPD_E_SHAPE, "recent %d out of range (0..budget)", recent);
   if ((long long)cache->layers * cache->batch * cache->kv_heads > 0x7fffffffLL) return fail(BPD_E_SHAPE, "layers * batch * kv_heads out of range");
   if ((rc = check_scratch(scratch, scratch_bytes, bpd_op_cache_evict_scratch_bytes(cache, budget)))) return rc;
+  const size_t per_row = (size_t)cache->batch * 4;
+  if ((rc = check_apart({{out_lens, per_row, "out_lens"}},
+                        {{lens, per_row, "lens"}, {seen, per_row, "seen"}, {cache->page_table, per_row * cache->pages_per_row, "the page table"}}))) return rc;
   EvictArgs a;
   a.k_pool = cache->k_pool; a.v_pool = cache->v_pool; a.table = cache->page_table; a.lens = lens; a.seen = seen; a.layers = cache->layers;
   a.B = cache->batch; a.Hkv = cache->kv_heads; a.row_pieces = cache->head_dim * elem_of(cache) / 16; a.ppr = cache->pages_per_row;

@@ -123,6 +123,23 @@ def test_commit_weights_and_eviction_refuse(b):
     assert _means(b, means=P + 4) == INVALID
 
 
+# every CTA of a sequence walks its tree by these arrays, whenever it starts: an output in their place would change the walk
+def test_commit_and_eviction_refuse_outputs_in_the_place_of_inputs(b):
+    spread = {name: (i + 2) * P for i, name in enumerate(("lens", "parents", "tokens", "top1", "last_top1", "n_nodes"))}
+    apart = {name: (i + 20) * P for i, name in enumerate(("out_lens", "accepted", "path", "following"))}
+    for out in apart:
+        for name, at in spread.items():
+            assert _commit(b, **{**spread, **apart, out: at}) == INVALID, (out, name)
+            assert b"overlap" in b.lib.bpd_last_error()
+        assert _commit(b, **{**spread, **apart, out: P}) == INVALID            # the page table
+    # parts of them: 2 sequences of 4 nodes
+    assert _commit(b, **{**spread, **apart, "path": spread["last_top1"] - 28}) == INVALID and _commit(b, **{**spread, **apart, "following": spread["top1"] + 28}) == INVALID
+    for name in ("lens", "seen"):
+        assert _evict(b, **{"lens": 5 * P, "seen": 6 * P, "out_lens": {"lens": 5 * P, "seen": 6 * P}[name] + 4}) == INVALID
+        assert b"overlap" in b.lib.bpd_last_error()
+    assert _evict(b, lens=5 * P, seen=6 * P, out_lens=P + 396) == INVALID      # the page table's last entry
+
+
 def test_scratch_grows_with_what_needs_it(b):
     n = b.lib.bpd_op_tree_attention_scratch_bytes(_cache(b), 4, 4)
     assert 0 < n < b.lib.bpd_op_tree_attention_scratch_bytes(_cache(b, batch=640), 64, 4)
