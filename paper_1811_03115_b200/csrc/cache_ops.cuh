@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kWThreads) cache_weights_kernel(const __grid_c
             s_step[r] = (r0 + r) / a.G;
           }
         } else if (c == 0) {
-          s_hi[r] = INFINITY; s_lo[r] = 0.f; s_step[r] = -1;         // weight 0
+          s_hi[r] = s_lo[r] = 0.f; s_step[r] = 0;                    // padding: add_up leaves these rows out
         }
         if constexpr (W::F32) {
           uint32_t x[3], y[3];
@@ -265,6 +265,10 @@ __global__ void __launch_bounds__(kWThreads) cache_weights_kernel(const __grid_c
             if (pos > len + step1) e[1] = 0.f;
             if (pos + 8 > len + step0) e[2] = 0.f;
             if (pos + 8 > len + step1) e[3] = 0.f;
+          }
+          if (n0 + 8 > n) {                                        // rows of padding: their zeros times an infinite key are no numbers
+            if (n0 + t4 * 2 >= n) e[0] = e[2] = 0.f;
+            if (n0 + t4 * 2 + 1 >= n) e[1] = e[3] = 0.f;
           }
           sum0 += e[0] + e[1];
           sum1 += e[2] + e[3];

@@ -283,6 +283,66 @@ def test_cache_weights(bpd, lens, nodes, heads, kv_heads, dim, dtype):
     assert np.array_equal(got_w.cpu().numpy()[untouched], weights[untouched])
 
 
+class WeightsCase(Case):
+    """A path of accepted nodes whose keys are in the cache, as a commit leaves them; lse in 64 bits, rounded."""
+
+    def __init__(self, seed, lens, accepted, nodes, heads, kv_heads, dim, dtype, change=lambda c: None):
+        super().__init__(seed, lens, nodes, heads, kv_heads, dim, dtype, tree="chain")
+        b, cap = len(lens), self.table.shape[1] * PAGE
+        self.accepted = np.asarray(accepted, np.int32)
+        self.path = np.full((b, nodes), -1, np.int32)
+        for r in range(b):
+            self.path[r, :accepted[r]] = np.sort(self.rng.permutation(nodes)[:accepted[r]])
+            for i in range(accepted[r]):
+                s = lens[r] + i
+                self.k[0, self.table[r, s // PAGE], s % PAGE] = self.k_new[0, r, self.path[r, i]]
+        change(self)
+        self.q = _round(self.q, dtype)                       # both sides get what the type holds
+        self.lse = np.full((b, nodes, heads), np.nan, np.float32)
+        for r in range(b):
+            for i in range(accepted[r]):
+                for g in range(heads):
+                    keys = plain.cached(self.k[0][:, :, g * kv_heads // heads], self.table[r], range(lens[r] + i + 1))
+                    self.lse[r, self.path[r, i], g] = plain.softmax_row(self.q[r, self.path[r, i], g].astype(np.float64), keys, keys, self.scale)[1]
+        self.weights = self.rng.random((b, kv_heads, cap)).astype(np.float32)
+        self.positions = self.rng.integers(0, 1000, (b, kv_heads, cap)).astype(np.int32)
+        self.seen = np.arange(b).astype(np.int32) * 1000 + 7
+
+    def check_weights(self, bpd):
+        want_w, want_p = plain.cache_weights(self.q, self.lse, self.path, self.accepted, self.k[0], self.table, self.lens, self.seen, self.weights,
+                                             self.positions, self.scale)
+        k, _, table = self.pools(0)
+        got_w, got_p = _dev(self.weights), _dev(self.positions)
+        bpd.bpd_op_cache_weights(_dev(self.q, self.dtype), _dev(self.lse), _dev(self.path), _dev(self.accepted), k, table, _dev(self.lens), _dev(self.seen),
+                                 got_w, got_p)
+        assert np.array_equal(got_p.cpu().numpy(), want_p)
+        # as in test_cache_weights: the score's error, the difference to lse, 2 units of the exponential, a rounding for each row of a sum
+        rows = int(self.accepted.max()) * self.heads // self.kv_heads
+        off = self.key_error() + 2.0 ** -24 * np.nanmax(np.abs(self.lse)) + 2.0 ** -21 + (rows + 2) * 2.0 ** -24
+        got = got_w.double().cpu().numpy()
+        assert not np.isnan(got).any()
+        assert (np.abs(got - want_w) <= off * (want_w + 1e-30) + 2.0 ** -23 * want_w).all()
+
+    def key_error(self):
+        """weight_error's first part over keys of ordinary size (those beyond give a weight of 0 or are set by hand)."""
+        keys = np.abs(np.concatenate([self.k.reshape(-1), self.k_new.reshape(-1)]))
+        keys = keys[keys < 100].max()
+        return self.scale * float(np.abs(self.q).sum(-1).max()) * float(keys) * (self.dim / 16 + 4) * 2.0 ** -23
+
+
+# A cached key with an infinite element whose products are all -inf has weight 0, whatever the number of rows (they are padded
+# to eight)
+@pytest.mark.parametrize("lens,accepted,nodes,heads,kv_heads,dim", [([100], [1], 1, 1, 1, 64), ([130, 70], [3, 2], 4, 6, 2, 128), ([200], [8], 9, 2, 2, 32),
+                                                                    ([90], [5], 5, 3, 1, 16), ([300], [9], 12, 8, 1, 64)])
+def test_cache_weights_of_infinite_keys(bpd, lens, accepted, nodes, heads, kv_heads, dim):
+    def change(c):
+        c.q[..., 3] = np.abs(c.q[..., 3]) + 0.25
+        for r, n in enumerate(lens):
+            for s in (0, 17, n - 1):
+                c.k[0, c.table[r, s // PAGE], s % PAGE, :, 3] = -np.inf
+    WeightsCase(dim, lens, accepted, nodes, heads, kv_heads, dim, "bf16", change).check_weights(bpd)
+
+
 EVICT = [(1, [1], 1, 16, 1, 0, "bf16"), (2, [65, 10, 64], 2, 32, 20, 5, "fp32"), (1, [522], 4, 64, 512, 64, "fp32"), (3, [700, 300], 2, 128, 100, 100, "bf16"),
          (1, [1500, 1], 3, 64, 1, 0, "bf16"), (2, [3000], 2, 16, 2999, 7, "bf16"), (1, [1024, 513, 512], 1, 32, 512, 0, "fp32"),
          # more slots than registers hold keys of
