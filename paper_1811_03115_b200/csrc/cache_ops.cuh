@@ -273,6 +273,34 @@ __global__ void __launch_bounds__(kWThreads) cache_weights_kernel(const __grid_c
           sum0 += e[0] + e[1];
           sum1 += e[2] + e[3];
         }
+        if constexpr (W::F32) {
+          // Planes hold numbers up to 3.39e38 only: larger ones and infinities (0 or not a number in the planes behind the first)
+          // make a score that is no number.  Such a tile's scores are taken again in 64 bits, from the numbers themselves.
+          if (__any_sync(0xffffffffu, sum0 != sum0 || sum1 != sum1)) {
+            sum0 = sum1 = 0.f;
+            for (int r = 0; r < n; ++r) {
+              const int node = clamp_int(a.path[(long long)b * a.T + (r0 + r) / a.G], 0, a.T - 1);
+              const float* src = reinterpret_cast<const float*>(a.q) + ((long long)b * a.T + node) * a.q_stride + (h * a.G + (r0 + r) % a.G) * D;
+              double c[2] = {0., 0.};
+#pragma unroll
+              for (int st = 0; st < W::STEPS; ++st)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                  const double x = src[(t4 + 4 * st) * VEC + e];
+#pragma unroll
+                  for (int half = 0; half < 2; ++half) c[half] += x * (double)__uint_as_float(keys.v[st][half][e]);
+                }
+              float w[2];
+#pragma unroll
+              for (int half = 0; half < 2; ++half) {
+                c[half] += __shfl_xor_sync(0xffffffffu, c[half], 1);
+                c[half] += __shfl_xor_sync(0xffffffffu, c[half], 2);
+                w[half] = pos0 + g + half * 8 > len + s_step[r] ? 0.f : exp2_fast((float)(c[half] * (double)a.scale_log2 - (double)s_hi[r] - (double)s_lo[r]));
+              }
+              if (t4 == 0) { sum0 += w[0]; sum1 += w[1]; }
+            }
+          }
+        }
         sum0 += __shfl_xor_sync(0xffffffffu, sum0, 1); sum0 += __shfl_xor_sync(0xffffffffu, sum0, 2);
         sum1 += __shfl_xor_sync(0xffffffffu, sum1, 1); sum1 += __shfl_xor_sync(0xffffffffu, sum1, 2);
         if (t4 < 2) {

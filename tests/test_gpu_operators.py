@@ -327,7 +327,8 @@ class WeightsCase(Case):
         """weight_error's first part over keys of ordinary size (those beyond give a weight of 0 or are set by hand)."""
         keys = np.abs(np.concatenate([self.k.reshape(-1), self.k_new.reshape(-1)]))
         keys = keys[keys < 100].max()
-        return self.scale * float(np.abs(self.q).sum(-1).max()) * float(keys) * (self.dim / 16 + 4) * 2.0 ** -23
+        q = np.where(np.abs(self.q) < 100, np.abs(self.q), 0)
+        return self.scale * float(q.sum(-1).max()) * float(keys) * (self.dim / 16 + 4) * 2.0 ** -23
 
 
 # A cached key with an infinite element whose products are all -inf has weight 0, whatever the number of rows (they are padded
@@ -341,6 +342,22 @@ def test_cache_weights_of_infinite_keys(bpd, lens, accepted, nodes, heads, kv_he
             for s in (0, 17, n - 1):
                 c.k[0, c.table[r, s // PAGE], s % PAGE, :, 3] = -np.inf
     WeightsCase(dim, lens, accepted, nodes, heads, kv_heads, dim, "bf16", change).check_weights(bpd)
+
+
+# The same in 32 bits, with the largest finite numbers too: among keys whose weight is 0 for them, and in a query against zeros
+@pytest.mark.parametrize("lens,accepted,nodes,heads,kv_heads,dim", [([100], [1], 1, 1, 1, 64), ([130, 70], [3, 2], 4, 6, 2, 128), ([200], [8], 9, 2, 2, 32),
+                                                                    ([90], [5], 5, 3, 1, 16), ([300], [9], 12, 8, 1, 64)])
+def test_cache_weights_of_the_largest_numbers(bpd, lens, accepted, nodes, heads, kv_heads, dim):
+    far = np.finfo(np.float32)
+
+    def change(c):
+        c.q[..., 3], c.q[..., 4] = np.abs(c.q[..., 3]) + 0.25, -np.abs(c.q[..., 4]) - 0.25
+        c.k[..., 5], c.k_new[..., 5] = 0, 0
+        for r, n in enumerate(lens):
+            c.q[r, c.path[r, accepted[r] - 1], :, 5] = far.max
+            for s, d, x in ((0, 3, -np.inf), (9, 3, far.min), (18, 4, far.max), (n // 2, 4, np.inf), (n // 2 + 1, 3, np.float32(-3.397e38)), (n - 1, 4, far.max)):
+                c.k[0, c.table[r, s // PAGE], s % PAGE, :, d] = x
+    WeightsCase(dim, lens, accepted, nodes, heads, kv_heads, dim, "fp32", change).check_weights(bpd)
 
 
 EVICT = [(1, [1], 1, 16, 1, 0, "bf16"), (2, [65, 10, 64], 2, 32, 20, 5, "fp32"), (1, [522], 4, 64, 512, 64, "fp32"), (3, [700, 300], 2, 128, 100, 100, "bf16"),
