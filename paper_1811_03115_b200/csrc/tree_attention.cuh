@@ -553,8 +553,9 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
         l1 += s[i][2] + s[i][3];
       }
 
-      // A masked node's values may be infinite or not numbers, and 0 times those is not 0: where the tree's chunk holds
-      // such values, its products are taken one by one, without the keys whose weight is 0.
+      // A masked node's values may be infinite or not numbers, and 0 times those is not 0 (in 32 bits, numbers too that the
+      // first plane rounds to infinity): where the tree's chunk holds such values, its products are taken one by one, without the
+      // keys whose weight is 0.
       bool odd = false;
       if (c >= cache_chunks) {
         int bad = 0;
@@ -562,7 +563,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
           const uint4 v = *reinterpret_cast<const uint4*>(vb + L::v_at(i / L::PIECES, i % L::PIECES));
           const uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) bad |= (x[e] & 0x7f800000u) == 0x7f800000u || (!F32 && (x[e] & 0x7f80u) == 0x7f80u);
+          for (int e = 0; e < 4; ++e)
+            bad |= F32 ? (x[e] & 0x7fffffffu) >= 0x7f7f8000u : (x[e] & 0x7f800000u) == 0x7f800000u || (x[e] & 0x7f80u) == 0x7f80u;
         }
         odd = __syncthreads_or(bad) != 0;
       }

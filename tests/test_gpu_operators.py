@@ -146,6 +146,22 @@ def test_values_that_are_no_numbers_stay_in_their_line(bpd, dtype, dim, nodes, l
     assert bool(out[:, 2].isnan().all()) and bool(out[:, 5, :, ::3].isnan().all()) and bool(out[:, 5, :, 1::3].isfinite().all())
 
 
+# the largest numbers of the type likewise; what sees them comes out as they are, times the weight
+@pytest.mark.parametrize("dim,nodes,length", [(64, 9, 10), (16, 20, 10), (128, 40, 0), (32, 70, 600)])
+def test_largest_values_stay_in_their_line(bpd, dim, nodes, length):
+    c = Case(13, [length, 0], nodes, 2, 1, dim, "fp32", tree="star")
+    bad, far = [2, nodes - 1], np.finfo(np.float32)
+    c.v_new[:, :, 2, :, ::3], c.v_new[:, :, nodes - 1, :, 1] = far.min, np.float32(3.397e38)
+    want, want_lse = plain.attention(c.q, c.k_new[0], c.v_new[0], c.k[0], c.v[0], c.table, c.lens, c.parents, c.nodes, c.scale)
+    out, lse = bpd.bpd_op_tree_attention(*c.drafted(), *c.pools(0), _dev(c.lens), _dev(c.parents), want_lse=True)
+    c.v_new = np.where(np.abs(c.v_new) < 100, c.v_new, 0)    # check's tolerance goes by the largest value that a row sees
+    fine = [t for t in range(nodes) if t not in bad]
+    c.check(out[:, fine], want[:, fine], want_lse[:, fine], lse[:, fine])
+    rest = sum(c.weight_error()) * 2 + 2.0 ** -22
+    for t, cols in ((2, slice(0, None, 3)), (nodes - 1, slice(1, 2))):
+        assert (np.abs(out[:, t, :, cols].double().cpu().numpy() / want[:, t, :, cols] - 1) <= rest).all()
+
+
 # pages outside the pool, parents that do not lie before their node, lengths and node counts outside their ranges
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_values_of_device_arrays_are_not_trusted(bpd, dtype):
