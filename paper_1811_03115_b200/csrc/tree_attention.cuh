@@ -353,7 +353,10 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
   if (!work) return;
   int lines_of = -1;                                        // sequence whose lines are in shared memory
   int n = 0;                                                // chunks so far
-  do {
+  // fp32: planes hold numbers up to 3.39e38 only, larger ones and infinities come out of the products as NaN.  A run of a tile's
+  // chunks that ends with such a row is done again `from_numbers`: scores in 64 bits, values by FMAs.
+  bool from_numbers = false;
+  for (bool more = true; more;) {
     const int rows = w.rows(), b = w.b, cache_chunks = w.cache_chunks(), c_begin = w.c_begin, c_end = w.c_end;
     auto node_of = [&](int r) { return w.node_of(r); };
     auto head_of = [&](int r) { return w.head_of(r); };
@@ -458,7 +461,22 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
       float s[NT][4];
 #pragma unroll
       for (int i = 0; i < NT; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
-      if constexpr (F32) {
+      if (F32 && from_numbers) {
+        const int ra = min(wr * 16 + g, rows - 1), rb = min(wr * 16 + g + 8, rows - 1);
+        const float* qa = reinterpret_cast<const float*>(a.q) + ((long long)b * a.T + node_of(ra)) * a.q_stride + head_of(ra) * D;
+        const float* qb = reinterpret_cast<const float*>(a.q) + ((long long)b * a.T + node_of(rb)) * a.q_stride + head_of(rb) * D;
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float* kr = reinterpret_cast<const float*>(kb) + (key0 + i * 8 + t4 * 2 + e) * L::KP;
+            double sa = 0., sb = 0.;
+#pragma unroll 1
+            for (int d = 0; d < D; ++d) { sa += (double)qa[d] * (double)kr[d]; sb += (double)qb[d] * (double)kr[d]; }
+            s[i][e] = (float)(sa * (double)a.scale_log2);
+            s[i][2 + e] = (float)(sb * (double)a.scale_log2);
+          }
+      } else if constexpr (F32) {
         // Products one behind the other go to different accumulators (J tiles of keys side by side): a chain on one of them
         // would wait for every product's latency (64 rows, heads of 64: 202 us instead of 156 over 8 sequences of 4000).
         constexpr int J = NT < 4 ? NT : 4;
@@ -504,10 +522,12 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
           }
         }
       }
+      if (!F32 || !from_numbers) {
 #pragma unroll
-      for (int i = 0; i < NT; ++i)
+        for (int i = 0; i < NT; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[i][j] *= a.scale_log2;
+          for (int j = 0; j < 4; ++j) s[i][j] *= a.scale_log2;
+      }
 
       // what the rows do not see
       if (c >= cache_chunks) {
@@ -568,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
         }
         odd = __syncthreads_or(bad) != 0;
       }
-      if (odd) {
+      if (odd || (F32 && from_numbers)) {
 #pragma unroll
         for (int n = 0; n < DT; ++n) { o[n][0] *= f0; o[n][1] *= f0; o[n][2] *= f1; o[n][3] *= f1; }
 #pragma unroll
@@ -656,9 +676,20 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
       }
     }
 
-    // join the warps that shared the rows
     asm volatile("cp.async.wait_all;" ::: "memory");
-    __syncthreads();                                        // the ring has been used
+    if constexpr (F32) {
+      bool no_number = l0 != l0 || l1 != l1;
+#pragma unroll
+      for (int n = 0; n < DT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) no_number |= o[n][e] != o[n][e];
+      from_numbers = __syncthreads_or(no_number && !from_numbers);   // (the ring has been used)
+      if (from_numbers) continue;
+    } else {
+      __syncthreads();
+    }
+
+    // join the warps that shared the rows
     l0 += __shfl_xor_sync(0xffffffffu, l0, 1); l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
     l1 += __shfl_xor_sync(0xffffffffu, l1, 1); l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
     float* mg = reinterpret_cast<float*>(ring);
@@ -703,7 +734,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
     if (!a.split) return;
     if (c_begin == 0 && tid == 0) a.info[tl.id] = make_int2(blockIdx.x * 2 + w.slot, w.last_cta);
     __syncthreads();                                        // the ring, the lines and the sums are free again
-  } while (w.next());
+    more = w.next();
+  }
 }
 
 // Joins the partial results of the tiles that more than one CTA worked on.  grid: (tiles that could be, rows / (4 / SHARE)):

@@ -162,6 +162,41 @@ def test_largest_values_stay_in_their_line(bpd, dim, nodes, length):
         assert (np.abs(out[:, t, :, cols].double().cpu().numpy() / want[:, t, :, cols] - 1) <= rest).all()
 
 
+# Infinities and the largest numbers that every row sees, in 32 bits: keys of weight 0 for them, a query's element that meets zeros,
+# values of both kinds.  Tiles of 16, 32 and 64 rows, whole and in runs, selected pages.
+@pytest.mark.parametrize("lens,nodes,heads,kv_heads,dim,select", [([70, 130], 1, 2, 2, 64, 0), ([900, 64], 5, 2, 1, 16, 0), ([2000], 20, 2, 2, 128, 0),
+                                                                  ([700, 100], 40, 2, 1, 32, 0), ([300], 70, 3, 1, 64, 0), ([1500], 3, 4, 2, 64, 30)])
+def test_tree_attention_of_the_largest_numbers(bpd, lens, nodes, heads, kv_heads, dim, select):
+    import torch
+    c = Case(17, lens, nodes, heads, kv_heads, dim, "fp32")
+    far = np.finfo(np.float32)
+    c.q[..., 3], c.q[..., 4] = np.abs(c.q[..., 3]) + 0.25, -np.abs(c.q[..., 4]) - 0.25
+    c.k[..., 5], c.k_new[..., 5], c.q[:, nodes // 2, :, 5] = 0, 0, far.max
+    for r, n in enumerate(lens):
+        at = lambda s: (0, c.table[r, s // PAGE], s % PAGE)
+        for s, d, x in ((0, 3, -np.inf), (9, 3, far.min), (18, 4, far.max), (n // 2, 4, np.inf), (n // 2 + 1, 3, np.float32(-3.397e38)), (n - 1, 4, far.max)):
+            c.k[at(s) + (slice(None), d)] = x
+        for s, d, x in ((1, 7, np.inf), (n // 2 + 2, 8, far.min), (n - 2, 9, np.float32(3.397e38)), (2, 10, -np.inf)):
+            c.v[at(s) + (slice(None), d)] = x
+    c.k_new[:, :, 0, :, 4] = far.max
+    d = c.drafted() + c.pools(0)
+    if select:
+        means = np.zeros((len(lens),) + c.table.shape[1:] + (kv_heads, dim), np.float32)
+        want, want_lse, _ = plain.page_attention(c.q, c.k_new[0], c.v_new[0], c.k[0], c.v[0], c.table, means, c.lens, c.parents, select, c.nodes, c.scale)
+        out, lse = bpd.bpd_op_page_attention(*d, _dev(means), _dev(c.lens), _dev(c.parents), select, want_lse=True)
+    else:
+        want, want_lse = plain.attention(c.q, c.k_new[0], c.v_new[0], c.k[0], c.v[0], c.table, c.lens, c.parents, c.nodes, c.scale)
+        out, lse = bpd.bpd_op_tree_attention(*d, _dev(c.lens), _dev(c.parents), want_lse=True)
+    c.q, c.k, c.v, c.k_new = (np.where(np.isnan(x) | (np.abs(x) < 100), x, 0) for x in (c.q, c.k, c.v, c.k_new))    # what check's tolerance goes by
+    rest = sum(c.weight_error()) * 2 + 2.0 ** -22
+    odd = np.zeros(dim, bool)
+    odd[7:11] = True
+    got = out.double().cpu().numpy()
+    assert np.array_equal(got[..., [7, 10]], want[..., [7, 10]]) and np.isinf(want[..., [7, 10]]).all()
+    assert (np.abs(got[..., 8:10] / want[..., 8:10] - 1) <= rest).all() and (np.abs(want[..., 8:10]) > 1e20).all()
+    c.check(out[..., torch.from_numpy(~odd).cuda()], want[..., ~odd], want_lse, lse)
+
+
 # pages outside the pool, parents that do not lie before their node, lengths and node counts outside their ranges
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_values_of_device_arrays_are_not_trusted(bpd, dtype):
