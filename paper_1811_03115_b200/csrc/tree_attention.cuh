@@ -575,7 +575,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
 
       // A masked node's values may be infinite or not numbers, and 0 times those is not 0 (in 32 bits, numbers too that the
       // first plane rounds to infinity): where the tree's chunk holds such values, its products are taken one by one, without the
-      // keys whose weight is 0.
+      // keys that the row does not see.
       bool odd = false;
       if (c >= cache_chunks) {
         int bad = 0;
@@ -591,6 +591,10 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
       if (odd || (F32 && from_numbers)) {
 #pragma unroll
         for (int n = 0; n < DT; ++n) { o[n][0] *= f0; o[n][1] *= f0; o[n][2] *= f1; o[n][3] *= f1; }
+        // (a weight may be 0 for a key that the row does see: 0 times what is no number is none)
+        const int ra = wr * 16 + g, rb = ra + 8;
+        const unsigned long long see0 = c < cache_chunks ? ~0ull : (ra < rows ? s_lines.bits[c - cache_chunks][node_of(ra)] : 0ull);
+        const unsigned long long see1 = c < cache_chunks ? ~0ull : (rb < rows ? s_lines.bits[c - cache_chunks][node_of(rb)] : 0ull);
 #pragma unroll
         for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -606,8 +610,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
                 float x;
                 if (F32) x = *reinterpret_cast<const float*>(vb + (r * L::VP + d) * 4);
                 else x = __bfloat162float(*reinterpret_cast<const bf16*>(vb + L::swz(r, d / 8) + (d % 8) * 2));
-                if (w0 != 0.f) o[n][e] = fmaf(w0, x, o[n][e]);
-                if (w1 != 0.f) o[n][2 + e] = fmaf(w1, x, o[n][2 + e]);
+                if ((see0 >> r) & 1) o[n][e] = fmaf(w0, x, o[n][e]);
+                if ((see1 >> r) & 1) o[n][2 + e] = fmaf(w1, x, o[n][2 + e]);
               }
           }
       } else if constexpr (F32) {
@@ -719,7 +723,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
         const float f = exp2f(s_m[w][r] - base);
         const float4 y = *reinterpret_cast<const float4*>(mg + (w * R + r) * S::MP + c4);
         l = fmaf(s_l[w][r], f, l);
-        if (f != 0.f) { x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w); }
+        x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
       }
       if (whole) {
         const float inv = l == 0.f ? 0.f : 1.f / l;

@@ -146,6 +146,21 @@ def test_values_that_are_no_numbers_stay_in_their_line(bpd, dtype, dim, nodes, l
     assert bool(out[:, 2].isnan().all()) and bool(out[:, 5, :, ::3].isnan().all()) and bool(out[:, 5, :, 1::3].isfinite().all())
 
 
+# and whoever does see them has no finite output there, even with a weight that is 0 in 32 bits
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dim,nodes,length", [(64, 9, 10), (128, 20, 0), (16, 40, 30), (64, 70, 300), (128, 100, 900)])
+def test_values_that_are_no_numbers_show_whatever_their_weight(bpd, dim, nodes, length, dtype):
+    c = Case(15, [length, 5], nodes, 2, 1, dim, dtype, tree="chain")
+    c.q[..., 3], c.k_new[..., 3] = 8, 8                      # scores of 64 times the scale and more, against -64 times 32: weights of 0
+    c.k_new[:, :, 2, :, 3] = -2048
+    c.v_new[:, :, 2, :, ::2], c.v_new[:, :, 2, :, 1] = np.inf, np.nan
+    out = bpd.bpd_op_tree_attention(*c.drafted(), *c.pools(0), _dev(c.lens), _dev(c.parents))
+    bad = np.zeros(dim, bool)
+    bad[::2], bad[1] = True, True
+    fine = out.isfinite().cpu().numpy()
+    assert not fine[:, 2:][..., bad].any() and fine[:, :2].all() and fine[..., ~bad].all()
+
+
 # the largest numbers of the type likewise; what sees them comes out as they are, times the weight
 @pytest.mark.parametrize("dim,nodes,length", [(64, 9, 10), (16, 20, 10), (128, 40, 0), (32, 70, 600)])
 def test_largest_values_stay_in_their_line(bpd, dim, nodes, length):
