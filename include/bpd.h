@@ -372,7 +372,8 @@ int bpd_op_tree_attention(const bpd_cache* cache, const void* q, const void* k_n
  * taken, -1 behind them), out_next [batch]: the prediction after the last node
  * taken, i.e. what the next step passes as last_top1 (keep two arrays and swap
  * them).  No output may overlap an input: every CTA of a sequence walks its tree
- * (BPD_E_INVALID). */
+ * (BPD_E_INVALID).  A row whose length is negative takes no node; out_lens is
+ * the clamped length. */
 int bpd_op_tree_commit(const bpd_cache* cache, const void* k_new, const void* v_new, int nodes, int64_t kv_stride,
                        const int32_t* lens, const int32_t* parents, const int32_t* tokens, const int32_t* top1,
                        const int32_t* last_top1, const int32_t* n_nodes, int32_t eos_id, int32_t* out_lens,

@@ -29,7 +29,8 @@ __global__ void __launch_bounds__(kCommitThreads) tree_commit_kernel(const __gri
   __shared__ int s_parent[kMaxNodes], s_token[kMaxNodes], s_top1[kMaxNodes], s_path[kMaxNodes], s_row[kMaxNodes], s_n;
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
   const int nodes = a.nodes ? clamp_int(a.nodes[b], 0, a.T) : a.T;
-  const int len = a.lens[b], room = (len < 0 || len > a.ppr * kPagePos) ? 0 : a.ppr * kPagePos - len;
+  // (a length that cannot be takes nothing: a path would be written over what is there)
+  const int cap = a.ppr * kPagePos, given = a.lens[b], len = clamp_int(given, 0, cap), room = given < 0 ? 0 : cap - len;
   for (int i = tid; i < nodes; i += kCommitThreads) {
     s_parent[i] = a.parents[(long long)b * a.T + i];
     s_token[i] = a.tokens[(long long)b * a.T + i];

@@ -349,6 +349,19 @@ def test_cache_weights(bpd, lens, nodes, heads, kv_heads, dim, dtype):
     assert np.array_equal(got_w.cpu().numpy()[untouched], weights[untouched])
 
 
+# a length outside the cache comes back as the other calls read it
+def test_tree_commit_clamps_lengths(bpd):
+    c = Case(4, [100, 100, 100, 100], 8, 1, 1, 16, "fp32", tree="chain")
+    c.table = c.table[:, :2].copy()
+    zeros = np.zeros((4, 8), np.int32)
+    k, v, table = c.pools()
+    before = k.clone(), v.clone()
+    got = bpd.bpd_op_tree_commit(_dev(c.k_new), _dev(c.v_new), k, v, table, _dev(np.array([-1, 129, -2 ** 31, 2 ** 31 - 1], np.int32)), _dev(c.parents),
+                                 _dev(zeros), _dev(zeros), _dev(zeros[:, 0]))
+    assert got[0].tolist() == [0, 128, 0, 128] and got[1].tolist() == [0] * 4 and bool((got[2] == -1).all())
+    assert all(bool(((x == y) | (x.isnan() & y.isnan())).all()) for x, y in zip((k, v), before))
+
+
 class WeightsCase(Case):
     """A path of accepted nodes whose keys are in the cache, as a commit leaves them; lse in 64 bits, rounded."""
 
