@@ -434,6 +434,12 @@ int bpd_op_page_attention(const bpd_cache* cache, const float* means, const void
  * hardware or a debugger).  Synchronises the stream. */
 int bpd_op_status(void* cuda_stream);
 
+/* Self test of the above, as bpd_debug_wait_timeout: enqueues one CTA that waits
+ * as those kernels do, on a barrier nothing ever arrives on, with a limit of about
+ * limit_us microseconds (1..2000000).  The wait gives up, and the next
+ * bpd_op_status reports it, once. */
+int bpd_debug_op_wait_timeout(int limit_us, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

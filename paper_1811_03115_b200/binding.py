@@ -97,6 +97,7 @@ _SIGS = {
     "bpd_op_page_attention": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i64, _i64, _vp, _vp, _vp, _i, C.c_float, _vp, _sz, _vp, _vp, _vp,
                                    _vp]),
     "bpd_op_status": (_i, [_vp]),
+    "bpd_debug_op_wait_timeout": (_i, [_i, _vp]),
     "bpd_op_linear": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _vp, _sz, _vp, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
@@ -606,3 +607,8 @@ def bpd_op_status():
     """Raises BpdError (BPD_E_TIMEOUT) if a bounded wait in a kernel of the operators above has expired on the current device since
     the last call.  Synchronises the current stream."""
     _check(lib.bpd_op_status(_stream()))
+
+
+def bpd_debug_op_wait_timeout(limit_us: int = 2000):
+    """Enqueues a wait that expires after about ``limit_us`` microseconds, for bpd_op_status to report once."""
+    _check(lib.bpd_debug_op_wait_timeout(limit_us, _stream()))

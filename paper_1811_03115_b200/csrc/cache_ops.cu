@@ -313,6 +313,11 @@ int bpd_op_cache_evict(const bpd_cache* cache, const int32_t* lens, const int32_
   return BPD_OK;
 }
 
+int bpd_debug_op_wait_timeout(int limit_us, void* cuda_stream) {
+  if (limit_us < 1 || limit_us > 2000000) return fail(BPD_E_INVALID, "limit_us = %d outside 1..2000000", limit_us);
+  return let_wait_expire(limit_us, (cudaStream_t)cuda_stream);
+}
+
 int bpd_op_status(void* cuda_stream) {
   int expired = 0;
   const int rc = take_wait_expired(&expired, (cudaStream_t)cuda_stream);

@@ -81,6 +81,15 @@ template <> int launch_attention<bf16>(const AttnArgs& a, bool paged, int D, con
   })
 }
 
+int let_wait_expire(int limit_us, cudaStream_t st) {
+  int khz = 0, dev = 0;
+  BPD_CUDA(cudaGetDevice(&dev));
+  BPD_CUDA(cudaDeviceGetAttribute(&khz, cudaDevAttrClockRate, dev));
+  BPD_CUDA(launch_k(op_wait_probe_kernel, dim3(1), dim3(32), 0, st, false, (unsigned long long)limit_us * (unsigned long long)khz / 1000ull));
+  ++g_launches;
+  return BPD_OK;
+}
+
 int take_wait_expired(int* expired, cudaStream_t st) {
   const int zero = 0;
   BPD_CUDA(cudaMemcpyFromSymbolAsync(expired, g_wait_expired, sizeof(int), 0, cudaMemcpyDeviceToHost, st));

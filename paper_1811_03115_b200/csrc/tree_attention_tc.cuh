@@ -12,8 +12,8 @@
 // swizzle); what lies behind a sequence's last key in its open page, or behind its last node in the tree's chunk, comes along
 // and is masked, its values zeroed in shared memory (0 times NaN is not 0).
 //
-// Every wait is bounded; on expiry the CTA notes it (see bpd_op_status), waits (bounded) for its copies and products in
-// flight, frees its tensor memory and returns.
+// Every wait is bounded; on expiry the CTA notes it (see bpd_op_status).  However it ends, the copies and products it has
+// issued are waited for (bounded) before its tensor memory is freed and it returns.
 //
 // What bounds it: 8 sequences of 8000 and 128 rows, heads of 128, move 268 MB in 70 us of the launch's 79 with the join -- 0.58
 // of the copy's rate; the tensor pipe is active 39 % of the time.  A chunk takes a CTA 3000 cycles: about 1000 exponentials and
@@ -47,7 +47,7 @@ struct TcShape {
 // A wait of some operator's kernel has expired on this device since it was last asked (see bpd_op_status).
 static __device__ int g_wait_expired;
 
-__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* dead) {
+__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* dead, unsigned long long limit = tc::kSpinCycles) {
   if (tc::mbar_try_wait(bar, parity)) return true;
   const unsigned long long t0 = clock64();
   for (;;) {
@@ -55,7 +55,7 @@ __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile
     for (int i = 0; i < 64; ++i)
       if (tc::mbar_try_wait(bar, parity)) return true;
     if (*dead) return false;
-    if ((unsigned long long)(clock64() - t0) > tc::kSpinCycles) {
+    if ((unsigned long long)(clock64() - t0) > limit) {
       *dead = 1;
       return false;
     }
@@ -123,6 +123,19 @@ __device__ __forceinline__ uint64_t value_desc(uint32_t saddr, int panel_bytes) 
   return d;
 }
 
+// One CTA whose wait for a barrier that nothing arrives on expires, and which then ends as the kernel below does.
+static __global__ void op_wait_probe_kernel(unsigned long long limit) {
+  __shared__ __align__(8) unsigned long long bar;
+  __shared__ int dead;
+  if (threadIdx.x == 0) {
+    dead = 0;
+    tc::mbar_init(s_addr(&bar), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    wait_bar(s_addr(&bar), 0, &dead, limit);
+    if (dead) g_wait_expired = 1;
+  }
+}
+
 template <int D, bool PAGED>
 __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ TcMaps maps) {
   using S = TcShape<D>;
@@ -132,7 +145,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
   const uint32_t base = (s_addr(tt_smem) + 1023u) & ~1023u;        // swizzled tiles need 1024-byte alignment
   uint8_t* gen = tt_smem + (base - s_addr(tt_smem));
   const uint32_t q_s = base, k_s = q_s + S::Q_BYTES, v_s = k_s + KK * S::KV_BYTES;
-  __shared__ __align__(8) unsigned long long s_bar[2 * (KK + KV) + 7];
+  __shared__ __align__(8) unsigned long long s_bar[2 * (KK + KV) + 8];
   __shared__ uint32_t s_tmem;
   __shared__ int s_dead, s_odd, s_keys[4];
   __shared__ Lines s_lines;
@@ -143,7 +156,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
   auto v_empty = [&](int n) { return bars + 8 * (2 * KK + KV + n % KV); };
   auto s_full = [&](int s) { return bars + 8 * (2 * (KK + KV) + s); };
   auto p_ready = [&](int s) { return bars + 8 * (2 * (KK + KV) + 2 + s); };
-  const uint32_t pv_done = bars + 8 * (2 * (KK + KV) + 4), q_ready = pv_done + 8, rows_bar = pv_done + 16;
+  const uint32_t pv_done = bars + 8 * (2 * (KK + KV) + 4), q_ready = pv_done + 8, rows_bar = pv_done + 16, end_bar = pv_done + 24;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   clear_dead_rows<bf16>(a, D);
@@ -158,6 +171,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
     tc::mbar_init(pv_done, 1);
     tc::mbar_init(q_ready, 4);
     tc::mbar_init(rows_bar, 4);
+    tc::mbar_init(end_bar, 1);
     s_dead = 0;
     s_odd = 0;                                                     // the last tile that had such values
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -210,11 +224,9 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
           break;
         }
       }
-      // after an expired wait: copies in flight land before the shared memory goes
-      if (*dead) {
-        for (int i = max(0, nk - KK); i < nk; ++i) tc::mbar_wait(k_full(i), (i / KK) & 1);
-        for (int i = max(0, nv - KV); i < nv; ++i) tc::mbar_wait(v_full(i), (i / KV) & 1);
-      }
+      // copies in flight land before the shared memory goes, whoever's wait expires (used up, they have landed)
+      for (int i = max(0, nk - KK); i < nk; ++i) tc::mbar_wait(k_full(i), (i / KK) & 1);
+      for (int i = max(0, nv - KV); i < nv; ++i) tc::mbar_wait(v_full(i), (i / KV) & 1);
     }
   } else if (warp == 5) {
     // ---- products
@@ -258,12 +270,9 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
         }
         ++tile;
       } while (ok && w.next());
-      if (!ok) {
-        // nothing may write tensor memory once it is freed: pv_done's next phase ends when all products have
-        tc::umma_commit(pv_done);
-        const unsigned long long t0 = clock64();
-        while (clock64() - t0 < 1000000ull) {}
-      }
+      // nothing may read shared memory or write tensor memory once they go: all products end first, whoever's wait has expired
+      tc::umma_commit(end_bar);
+      tc::mbar_wait(end_bar, 0);
     }
   } else {
     // ---- softmax: a thread per row

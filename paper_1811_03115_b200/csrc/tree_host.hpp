@@ -98,6 +98,8 @@ int by_rows(const AttnArgs& a, bool paged, F&& f) {
 
 // Whether a wait of an operator's kernel has expired on the current device since it was last asked.
 int take_wait_expired(int* expired, cudaStream_t st);
+// A launch whose wait expires after so long (a self test).
+int let_wait_expire(int limit_us, cudaStream_t st);
 
 }  // namespace tree
 }  // namespace bpd

@@ -515,6 +515,20 @@ def test_two_streams_do_not_meet(bpd):
     bpd.bpd_op_status()                                      # no wait has expired
 
 
+# a wait that expires is reported once, and what follows is right
+def test_an_expired_wait_is_reported(bpd):
+    c = Case(25, [700, 90], 40, 4, 2, 128, "bf16")
+    args = c.drafted() + c.pools(0) + (_dev(c.lens), _dev(c.parents))
+    bpd.bpd_op_status()
+    first = bpd.bpd_op_tree_attention(*args)
+    bpd.bpd_debug_op_wait_timeout(2000)
+    again = bpd.bpd_op_tree_attention(*args)
+    with pytest.raises(bpd.BpdError, match="expired"):
+        bpd.bpd_op_status()
+    bpd.bpd_op_status()
+    assert bool((first == again).all())
+
+
 # a program's step: attention over the cache and the tree, commit, weights, eviction, and the next step's attention over what is
 # left, eagerly and as one captured graph replayed on another stream
 def _steps(bpd, c, state, budget):

@@ -148,6 +148,10 @@ def test_scratch_grows_with_what_needs_it(b):
     assert b.lib.bpd_op_cache_evict_scratch_bytes(_cache(b), 10 ** 9) == b.lib.bpd_op_cache_evict_scratch_bytes(_cache(b), 3200)
 
 
+def test_expiring_wait_refuses_limits(b):
+    assert b.lib.bpd_debug_op_wait_timeout(0, None) == INVALID and b.lib.bpd_debug_op_wait_timeout(2000001, None) == INVALID
+
+
 def test_binding_refuses_tensors(b):
     import torch
     k = torch.zeros(10, 64, 2, 64)
