@@ -228,6 +228,35 @@ def test_division_of_work(tmp_path):
     assert subprocess.run([str(tmp_path / "work")], capture_output=True, text=True).stdout == "ok\n"
 
 
+# The doubling of find_lines, lane by lane in the orders that a warp's lanes may take between two synchronisations: a lane that
+# stores its next round's state while another is between its two reads makes that one skip a part of its line.
+def test_lines_by_doubling_need_a_synchronisation_behind_their_reads():
+    rng = np.random.default_rng(3)
+
+    def doubled(parents, synchronised):
+        n = len(parents)
+        mine, mine_up = [1 << t for t in range(n)], [p if 0 <= p < t else -1 for t, p in enumerate(parents)]
+        bits, up = list(mine), list(mine_up)
+        while any(u >= 0 for u in mine_up):
+            bits, up = list(mine), list(mine_up)
+            order = rng.permutation(n)
+            for i, t in enumerate(order):
+                if mine_up[t] < 0:
+                    continue
+                seen = bits[mine_up[t]]
+                if not synchronised:
+                    for ahead in order[:i]:                  # these have done their reads
+                        bits[ahead], up[ahead] = mine[ahead], mine_up[ahead]
+                mine[t], mine_up[t] = mine[t] | seen, up[mine_up[t]]
+        return mine
+    parents = [max(-1, t - 1 - int(rng.integers(0, 3))) for t in range(60)]
+    want = [sum(1 << u for u in plain.line_of(parents, t)) for t in range(60)]
+    assert doubled(parents, True) == want and doubled(parents, False) != want
+    source = open(os.path.join(CSRC, "tree_attention.cuh")).read()
+    rounds = source[source.index("for (int reach = 1"):source.index("void find_lines")]
+    assert rounds.count("__syncwarp()") == 3                 # behind a round's stores, behind its reads, behind the last round
+
+
 # ---------------------------------------------------------------------- the oracle
 def test_oracle_attention_is_masked_attention():
     rng = np.random.default_rng(1)
