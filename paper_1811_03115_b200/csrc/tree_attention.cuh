@@ -88,7 +88,11 @@ struct Shape {
   static constexpr int STAGES = F32 ? (D >= 64 ? 2 : 3) : (D >= 128 ? 3 : 4);
   static constexpr int RING = STAGES * Rows<CT, D>::STAGE;
   static constexpr int SMEM = Q_BYTES + (RING > MERGE ? RING : MERGE);
-  static constexpr int CTAS_PER_SM = F32 ? (D >= 128 ? 1 : (WR < 4 ? 3 : 2)) : (D >= 128 ? 2 : 3);
+  // as many as shared memory holds (see tree_attention_kernel); the launch divides the work among all of them
+  static constexpr int CTAS_PER_SM = F32 ? (D >= 128 ? 1 : (D >= 64 || WR >= 4 ? 2 : 3)) : (D >= 128 ? 2 : 3);
+  // Registers of a third CTA are left free where two leave shared memory too: the joining launch's CTAs then wait on the same SMs
+  // (32 rows, 2 heads of 64 over 4 x 2000 positions: 13.8 us, with all registers taken 15.6; with 8 heads over 8 x 4000: 65.9 / 65.3).
+  static constexpr bool REGISTERS_FOR_JOIN = F32 && D == 64 && WR < 4;
 };
 
 // The nodes' lines as bits: bits[word][t] has those of node t's line among nodes 64 * word ..  By doubling: a node takes over
@@ -331,7 +335,7 @@ __device__ __forceinline__ void clear_dead_rows(const AttnArgs& a, int D) {
 // (With the pages of bf16 caches brought by TMA instead of every thread's 16-byte copies, the times were the same to 2 %, and
 // the tensor maps cost the host a microsecond a call.)
 template <typename CT, int D, int WR, bool PAGED>
-__global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tree_attention_kernel(const __grid_constant__ AttnArgs a) {
+__global__ void __launch_bounds__(kThreads, (!PAGED && Shape<CT, D, WR>::REGISTERS_FOR_JOIN ? 3 : Shape<CT, D, WR>::CTAS_PER_SM)) tree_attention_kernel(const __grid_constant__ AttnArgs a) {
   using S = Shape<CT, D, WR>;
   using L = Rows<CT, D>;
   pdl_launch_dependents();
@@ -341,6 +345,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<CT, D, WR>::CTAS_PER_SM)) tre
   __shared__ int s_keys[S::STAGES], s_pages[kPagesAhead];
   __shared__ Lines s_lines;
   __shared__ float s_m[WK][R], s_l[WK][R];
+  static_assert(S::CTAS_PER_SM * (S::SMEM + sizeof(s_keys) + sizeof(s_pages) + sizeof(s_lines) + sizeof(s_m) + sizeof(s_l) + 1024) <= 228 * 1024,
+                "the CTAs that share an SM do not fit its shared memory (1 KB of it is the system's, per CTA)");
   bf16* qs = reinterpret_cast<bf16*>(ta_smem);
   uint8_t* ring = ta_smem + S::Q_BYTES;
   const uint32_t ring_s = s_addr(ring);
