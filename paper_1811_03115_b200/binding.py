@@ -12,9 +12,21 @@ from dataclasses import dataclass
 from typing import Optional
 
 import numpy as np
-import torch
 
 from .build import LIB_PATH
+
+
+class _Torch:
+    """Stands for torch until its first use: sizes, error texts and the raw library need none.  (An import statement in each of the
+    operators on a paged cache would cost the smallest of them half a microsecond a call.)"""
+
+    def __getattr__(self, name):
+        import torch as module
+        globals()["torch"] = module
+        return getattr(module, name)
+
+
+torch = _Torch()
 
 BPD_MAX_K = 16
 BPD_OK = 0

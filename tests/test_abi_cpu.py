@@ -110,3 +110,17 @@ def test_top1_scratch_of_a_captured_call_is_its_own(lib, monkeypatch):
     assert captured[1] != kept[1] and captured[2] >= 512
     larger = lib._scratch_for(cpu, 6, 1024, True)
     assert larger[2] >= 1024 and list(lib._top1_scratch) == [(cpu, 5)] and lib._top1_scratch[(cpu, 5)][1] == kept[1]
+
+
+def test_sizes_need_no_torch(lib, tmp_path):
+    """The library, its error texts and the calls that look at host memory only load where torch is missing."""
+    import subprocess
+    import sys
+    make_weights(ModelConfig(1, 1, 32, 2, 64, 40, 3, 48, dtype=DTYPE_F32), 1, 0.1).tofile(tmp_path / "blob")
+    code = """import sys
+sys.modules['torch'] = None                                  # an import of it fails
+import numpy as np
+from paper_1811_03115_b200 import bpd_query_sizes, lib
+print(bpd_query_sizes(np.fromfile(sys.argv[1], np.uint8), 1, 8, 8)[0] > 0, lib.bpd_kernel_launches())"""
+    done = subprocess.run([sys.executable, "-c", code, str(tmp_path / "blob")], cwd=ROOT, capture_output=True, text=True)
+    assert done.stdout.split() == ["True", "0"], done.stderr[-2000:]
