@@ -100,6 +100,10 @@ int check_attention(const bpd_cache* c, const void* q, const void* k_new, const 
       (rc = check_rows(c, v_new, kv_stride, (long long)c->kv_heads * c->head_dim, "v_new"))) return rc;
   return BPD_OK;
 }
+int check_lists(const bpd_cache* c) {
+  if ((long long)c->layers * c->batch * c->kv_heads > 0x7fffffffLL) return fail(BPD_E_SHAPE, "layers * batch * kv_heads out of range");
+  return BPD_OK;
+}
 // The most entries of a list that an eviction moves: from above the budget to below it.
 int moves_cap(const bpd_cache* c, int budget) { return std::max(1, std::min(budget, c->pages_per_row * kPagePos - std::min(budget, c->pages_per_row * kPagePos))); }
 
@@ -159,7 +163,7 @@ using namespace bpd::tree;
 extern "C" {
 
 size_t bpd_op_tree_attention_scratch_bytes(const bpd_cache* cache, int nodes, int heads) {
-  if (check_cache(cache, false) || check_nodes(nodes) || check_heads(cache, heads)) return 0;
+  if (check_cache(cache, true) || check_nodes(nodes) || check_heads(cache, heads)) return 0;
   AttnPlan plan;
   if (plan_of(cache, attn_args(cache, nodes, heads, 0), false, &plan)) return 0;
   return plan.part_bytes + plan.info_bytes;
@@ -194,7 +198,7 @@ int bpd_op_page_means(const bpd_cache* cache, const int32_t* lens_from, const in
 }
 
 size_t bpd_op_page_attention_scratch_bytes(const bpd_cache* cache, int nodes, int heads, int select) {
-  if (check_cache(cache, false) || check_nodes(nodes) || check_heads(cache, heads) || select < 1 || select > cache->pages_per_row) return 0;
+  if (check_cache(cache, true) || check_nodes(nodes) || check_heads(cache, heads) || select < 1 || select > cache->pages_per_row) return 0;
   AttnPlan plan;
   if (plan_of(cache, attn_args(cache, nodes, heads, select), true, &plan)) return 0;
   const PagedSizes s = paged_sizes(cache, nodes, select);
@@ -274,7 +278,7 @@ int bpd_op_cache_weights(const bpd_cache* cache, const void* q, int nodes, int h
 }
 
 size_t bpd_op_cache_evict_scratch_bytes(const bpd_cache* cache, int budget) {
-  if (check_cache(cache, true) || budget < 1) return 0;
+  if (check_cache(cache, true) || check_lists(cache) || budget < 1) return 0;
   const size_t lists = (size_t)cache->layers * cache->batch * cache->kv_heads;
   return round256(lists * moves_cap(cache, budget) * 8) + round256(lists * 4);
 }
@@ -286,7 +290,7 @@ int bpd_op_cache_evict(const bpd_cache* cache, const int32_t* lens, const int32_
   if (!lens || !seen || !weights || !positions || !out_lens) return fail(BPD_E_INVALID, "null argument");
   if (budget < 1) return fail(BPD_E_SHAPE, "budget %d must be at least 1", budget);
   if (recent < 0 || recent > budget) return fail(BPD_E_SHAPE, "recent %d out of range (0..budget)", recent);
-  if ((long long)cache->layers * cache->batch * cache->kv_heads > 0x7fffffffLL) return fail(BPD_E_SHAPE, "layers * batch * kv_heads out of range");
+  if ((rc = check_lists(cache))) return rc;
   if ((rc = check_scratch(scratch, scratch_bytes, bpd_op_cache_evict_scratch_bytes(cache, budget)))) return rc;
   const size_t per_row = (size_t)cache->batch * 4;
   if ((rc = check_apart({{out_lens, per_row, "out_lens"}},

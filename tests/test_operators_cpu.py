@@ -148,6 +148,14 @@ def test_scratch_grows_with_what_needs_it(b):
     assert b.lib.bpd_op_cache_evict_scratch_bytes(_cache(b), 10 ** 9) == b.lib.bpd_op_cache_evict_scratch_bytes(_cache(b), 3200)
 
 
+def test_scratch_of_refused_calls_is_none(b):
+    many = dict(layers=65535, batch=65535, kv_heads=1024)
+    assert _evict(b, cache=_cache(b, **many)) == SHAPE and b.lib.bpd_op_cache_evict_scratch_bytes(_cache(b, **many), 5) == 0
+    for over in ({"v_pool": None}, {"v_pool": P + 8}, {"batch": 0}):
+        assert b.lib.bpd_op_tree_attention_scratch_bytes(_cache(b, **over), 4, 4) == 0 and b.lib.bpd_op_cache_evict_scratch_bytes(_cache(b, **over), 5) == 0
+        assert b.lib.bpd_op_page_attention_scratch_bytes(_cache(b, **over), 4, 4, 2) == 0
+
+
 def test_expiring_wait_refuses_limits(b):
     assert b.lib.bpd_debug_op_wait_timeout(0, None) == INVALID and b.lib.bpd_debug_op_wait_timeout(2000001, None) == INVALID
 
