@@ -469,6 +469,186 @@ def test_cache_evict(bpd, layers, lens, kv_heads, dim, budget, recent, dtype, ki
         assert np.array_equal(x.float().cpu().numpy(), np.asarray(y, np.float32), equal_nan=True)
 
 
+# ---------------------------------------------------------------------- runs of many turns, other layouts, the ends of the ranges
+def _far(seed, lens, nodes, heads, kv_heads, dim, dtype):
+    """Tensors of a long cache on the device, and bounds as Case.check takes them."""
+    import torch
+    gen = torch.Generator("cuda").manual_seed(seed)
+    dt, b = (torch.bfloat16 if dtype == "bf16" else torch.float32), len(lens)
+    ppr = -(-(max(lens) + nodes) // PAGE)
+    t = {n: torch.empty(s, dtype=dt, device="cuda").normal_(generator=gen) for n, s in
+         (("k", (b * ppr, PAGE, kv_heads, dim)), ("v", (b * ppr, PAGE, kv_heads, dim)), ("q", (b, nodes, heads, dim)), ("k_new", (b, nodes, kv_heads, dim)),
+          ("v_new", (b, nodes, kv_heads, dim)))}
+    t["table"] = torch.randperm(b * ppr, generator=gen, device="cuda").view(b, ppr).int()
+    t["lens"] = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    t["parents"] = (torch.arange(nodes, device="cuda") - 1).expand(b, nodes).int().contiguous()
+    return t
+
+
+# A CTA's run of more chunks than it looks up pages for at once (64): 444 CTAs share 2 x 8 x 3750 of them, and 296 share more than
+# 64 each in the others; tiles of 16, 32, 64 and 128 rows
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens,nodes,heads,kv_heads,dim", [([239963, 200001], 3, 8, 8, 16), ([239963, 200001], 4, 48, 8, 16), ([100000, 160001], 9, 24, 4, 32),
+                                                           ([150003] * 3, 40, 8, 4, 64)])
+def test_tree_attention_of_long_runs(bpd, lens, nodes, heads, kv_heads, dim, dtype):
+    import torch
+    t = _far(41, lens, nodes, heads, kv_heads, dim, dtype)
+    out, lse = bpd.bpd_op_tree_attention(t["q"], t["k_new"], t["v_new"], t["k"], t["v"], t["table"], t["lens"], t["parents"], want_lse=True)
+    scale, g = dim ** -0.5, heads // kv_heads
+    # as Case.weight_error
+    score = scale * float(t["q"].double().abs().sum(-1).max()) * float(torch.stack([t[n].abs().max() for n in ("k", "k_new")]).max()) * (dim / 16 + 4) * 2.0 ** -23
+    rest = 2.0 ** -21 + (2.0 ** -17 if dtype == "bf16" else 2.0 ** -22) + 4 * (max(lens) / 64 + 8) * 2.0 ** -24
+    top = float(torch.stack([t[n].abs().max() for n in ("v", "v_new")]).max())
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -23
+    tree = torch.ones(nodes, nodes, dtype=torch.bool, device="cuda").tril()
+    for b, n in enumerate(lens):
+        pages = t["table"][b].long()
+        for h in range(kv_heads):
+            keys, values = (torch.cat([t[p][pages, :, h].reshape(-1, dim)[:n], t[p + "_new"][b, :, h]]).double() for p in ("k", "v"))
+            q = t["q"][b, :, h * g:(h + 1) * g].double()
+            s = q @ keys.T * scale
+            s[..., n:].masked_fill_(~tree[:, None, :], -torch.inf)
+            want, want_lse = torch.softmax(s, -1) @ values, torch.logsumexp(s, -1)
+            got = out[b, :, h * g:(h + 1) * g].double()
+            assert bool(((got - want).abs() <= 2 * (score + rest) * top + half * want.abs()).all())
+            assert bool(((lse[b, :, h * g:(h + 1) * g].double() - want_lse).abs() <= score + rest + 2.0 ** -22 * want_lse.abs() + 2.0 ** -21).all())
+
+
+# Warps that take several tiles of a page run, runs that go on with another key head and another sequence, sequences that accepted
+# nothing among them: 2700 pages for 296 CTAs
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("kv_heads,heads,dim", [(2, 2, 64), (2, 6, 16), (1, 2, 128)])
+def test_cache_weights_of_long_runs(bpd, kv_heads, heads, dim, dtype):
+    few = 1 if kv_heads == 2 else 2
+    lens = [6400, 6399 * few, 1, 0, 12801 * few, 5000, 64, 9000 * few, 63, 7777, 12800 * few, 4095, 3]
+    accepted = [3, 1, 4, 2, 1, 0, 4, 2, 0, 4, 3, 1, 0]
+    WeightsCase(51, lens, accepted, 4, heads, kv_heads, dim, dtype).check_weights(bpd)
+
+
+# more columns than a CTA's threads take at once
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("kv_heads,dim", [(32, 128), (65, 64), (300, 16)])
+def test_page_means_of_wide_rows(bpd, kv_heads, dim, dtype):
+    import torch
+    c = Case(53, [200, 64], 1, kv_heads, kv_heads, dim, dtype, layers=2)
+    k, _, table = c.pools()
+    held = torch.full((2,) + c.table.shape + (kv_heads, dim), float("nan"), device="cuda")
+    bpd.bpd_op_page_means(k, table, _dev(np.zeros(2, np.int32)), _dev(c.lens), held)
+    for layer in range(2):
+        want, got = plain.page_means(c.k[layer], c.table, c.lens), held[layer].cpu().numpy()
+        assert np.array_equal(np.isnan(got), np.isnan(want))
+        np.testing.assert_allclose(np.nan_to_num(got), np.nan_to_num(want), rtol=2.0 ** -23)
+
+
+def _fused(*parts):
+    """The tensors [..., heads, dim] as slices of one row each, with NaN between and behind them."""
+    import torch
+    rows = [p.flatten(-2) for p in parts]
+    row = torch.full(rows[0].shape[:-1] + (sum(r.shape[-1] + 16 for r in rows) + 24,), float("nan"), device="cuda", dtype=rows[0].dtype)
+    at, out = 8, []
+    for p, r in zip(parts, rows):
+        row[..., at:at + r.shape[-1]] = r
+        out.append(row[..., at:at + r.shape[-1]].unflatten(-1, p.shape[-2:]))
+        at += r.shape[-1] + 16
+    assert row.shape[:-1].numel() == 1 or not any(o.is_contiguous() for o in out)
+    return out
+
+
+# every kernel that reads rows of drafted nodes, with rows further apart than they are wide: whole tiles and runs, few and many rows,
+# the selection for one node and for several
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens,nodes,heads,kv_heads,dim,select", [([70], 1, 4, 4, 32, 0), ([900, 1300], 5, 4, 2, 64, 0), ([900, 10], 33, 4, 2, 128, 0), ([700, 900], 70, 2, 1, 64, 0),
+                                                                  ([800, 1], 70, 4, 2, 128, 0), ([1500, 700], 1, 4, 2, 64, 9), ([1500], 6, 80, 1, 128, 9), ([2000, 65], 5, 6, 3, 16, 4)])
+def test_rows_further_apart_than_wide(bpd, lens, nodes, heads, kv_heads, dim, select, dtype):
+    import torch
+    c = Case(55, lens, nodes, heads, kv_heads, dim, dtype, live=[nodes] + [max(1, nodes - 2)] * (len(lens) - 1))
+    k, v, table = c.pools(0)
+    rest = (_dev(c.lens), _dev(c.parents))
+    means = torch.zeros((1,) + c.table.shape + (kv_heads, dim), device="cuda")
+    bpd.bpd_op_page_means(k[None], table, torch.zeros_like(rest[0]), rest[0], means)
+
+    def call(q, k_new, v_new):
+        if select:
+            return bpd.bpd_op_page_attention(q, k_new, v_new, k, v, table, means[0], *rest, select, nodes=_dev(c.nodes), want_lse=True, want_pages=True)
+        return bpd.bpd_op_tree_attention(q, k_new, v_new, k, v, table, *rest, nodes=_dev(c.nodes), want_lse=True)
+    for x, y in zip(call(*c.drafted()), call(*_fused(*c.drafted()))):
+        assert bool((x == y).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_commit_and_weights_of_rows_further_apart_than_wide(bpd, dtype):
+    c = WeightsCase(57, [130, 62, 700], [3, 5, 2], 7, 6, 2, 64, dtype)
+    k, _, table = c.pools(0)
+
+    def weights(q):
+        w, p = _dev(c.weights), _dev(c.positions)
+        bpd.bpd_op_cache_weights(q, _dev(c.lse), _dev(c.path), _dev(c.accepted), k, table, _dev(c.lens), _dev(c.seen), w, p)
+        return w, p
+    q = _dev(c.q, dtype)
+    for x, y in zip(weights(q), weights(_fused(q)[0])):
+        assert bool((x == y).all())
+    layers = Case(58, [130, 62, 5], 7, 2, 2, 64, dtype, layers=3, tree="chain")
+    zeros = np.zeros((3, 7), np.int32)
+
+    def commit(k_new, v_new):
+        k, v, table = layers.pools()
+        got = bpd.bpd_op_tree_commit(k_new, v_new, k, v, table, _dev(layers.lens), _dev(layers.parents), _dev(zeros), _dev(zeros), _dev(zeros[:, 0]))
+        return got + (k, v)
+    rows = _dev(layers.k_new, dtype), _dev(layers.v_new, dtype)
+    for x, y in zip(commit(*rows), commit(*_fused(*rows))):
+        assert bool(((x == y) | (x.isnan() & y.isnan())).all())
+
+
+# rows that share the pages of a common beginning, each with an open page of its own
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("nodes,dim", [(3, 64), (70, 128)])
+def test_sequences_that_share_pages(bpd, nodes, dim, dtype):
+    c = Case(59, [700, 660, 643], nodes, 2, 1, dim, dtype)
+    c.table[1, :10] = c.table[2, :10] = c.table[0, :10]
+    out, lse = bpd.bpd_op_tree_attention(*c.drafted(), *c.pools(0), _dev(c.lens), _dev(c.parents), want_lse=True)
+    c.check(out, *plain.attention(c.q, c.k_new[0], c.v_new[0], c.k[0], c.v[0], c.table, c.lens, c.parents, c.nodes, c.scale), lse)
+
+
+# a batch of nothing but padding; far more heads to a key head than a tile has rows; many sequences; many key heads
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens,nodes,heads,kv_heads,dim,select", [([70, 5], 3, 2, 2, 64, 0), ([700, 5], 3, 2, 2, 64, 0), ([700, 5], 40, 4, 2, 128, 0), ([700, 5], 3, 2, 2, 64, 4)])
+def test_a_batch_of_padding(bpd, lens, nodes, heads, kv_heads, dim, select, dtype):
+    import torch
+    c = Case(61, lens, nodes, heads, kv_heads, dim, dtype)
+    none = torch.zeros(len(lens), dtype=torch.int32, device="cuda")
+    args = c.drafted() + c.pools(0)
+    if select:
+        means = torch.zeros(c.table.shape + (kv_heads, dim), device="cuda")
+        out, lse, pages = bpd.bpd_op_page_attention(*args, means, _dev(c.lens), _dev(c.parents), select, nodes=none, want_lse=True, want_pages=True)
+        assert bool((pages == -1).all())
+    else:
+        out, lse = bpd.bpd_op_tree_attention(*args, _dev(c.lens), _dev(c.parents), nodes=none, want_lse=True)
+    assert bool((out == 0).all()) and bool(lse.isneginf().all())
+    k, v, table = c.pools()
+    zeros = torch.zeros(len(lens), nodes, dtype=torch.int32, device="cuda")
+    got = bpd.bpd_op_tree_commit(_dev(c.k_new, dtype), _dev(c.v_new, dtype), k, v, table, _dev(c.lens), _dev(c.parents), zeros, zeros, none + 9, nodes=none)
+    assert got[0].tolist() == lens and not bool(got[1].any()) and bool((got[2] == -1).all()) and bool((got[3] == 9).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens,nodes,heads,kv_heads,dim,select", [([300], 2, 300, 1, 64, 0), ([900], 1, 300, 1, 128, 5), ([500, 3], 2, 200, 1, 16, 3), ([3] * 700, 1, 1, 1, 16, 0),
+                                                                  ([2] * 699 + [900], 2, 2, 1, 32, 0), ([70], 1, 1024, 1024, 16, 0), ([450], 2, 600, 300, 32, 3)])
+def test_many_heads_and_many_sequences(bpd, lens, nodes, heads, kv_heads, dim, select, dtype):
+    import torch
+    c = Case(63, lens, nodes, heads, kv_heads, dim, dtype)
+    k, v, table = c.pools(0)
+    if select:
+        held = torch.zeros((1,) + c.table.shape + (kv_heads, dim), device="cuda")
+        bpd.bpd_op_page_means(k[None], table, _dev(np.zeros_like(c.lens)), _dev(c.lens), held)
+        want, want_lse, pages = plain.page_attention(c.q, c.k_new[0], c.v_new[0], c.k[0], c.v[0], c.table, held[0].cpu().numpy(), c.lens, c.parents, select, c.nodes, c.scale)
+        out, lse, chosen = bpd.bpd_op_page_attention(*c.drafted(), k, v, table, held[0], _dev(c.lens), _dev(c.parents), select, want_lse=True, want_pages=True)
+        assert np.array_equal(chosen.cpu().numpy(), pages)
+    else:
+        want, want_lse = plain.attention(c.q, c.k_new[0], c.v_new[0], c.k[0], c.v[0], c.table, c.lens, c.parents, c.nodes, c.scale)
+        out, lse = bpd.bpd_op_tree_attention(*c.drafted(), k, v, table, _dev(c.lens), _dev(c.parents), want_lse=True)
+    c.check(out, want, want_lse, lse)
+
+
 # what a race would show: the same call fifty times, with other work on the device between; many short runs that end and begin
 # inside tiles, and long ones
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
