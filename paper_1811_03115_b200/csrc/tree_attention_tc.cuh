@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
   const uint32_t base = (s_addr(tt_smem) + 1023u) & ~1023u;        // swizzled tiles need 1024-byte alignment
   uint8_t* gen = tt_smem + (base - s_addr(tt_smem));
   const uint32_t q_s = base, k_s = q_s + S::Q_BYTES, v_s = k_s + KK * S::KV_BYTES;
-  __shared__ __align__(8) unsigned long long s_bar[2 * (KK + KV) + 8];
+  __shared__ __align__(8) unsigned long long s_bar[2 * (KK + KV) + 9];
   __shared__ uint32_t s_tmem;
   __shared__ int s_dead, s_odd, s_keys[4];
   __shared__ Lines s_lines;
@@ -156,7 +156,10 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
   auto v_empty = [&](int n) { return bars + 8 * (2 * KK + KV + n % KV); };
   auto s_full = [&](int s) { return bars + 8 * (2 * (KK + KV) + s); };
   auto p_ready = [&](int s) { return bars + 8 * (2 * (KK + KV) + 2 + s); };
-  const uint32_t pv_done = bars + 8 * (2 * (KK + KV) + 4), q_ready = pv_done + 8, rows_bar = pv_done + 16, end_bar = pv_done + 24;
+  // Two, taken in turn, as for scores and weights: a wait by parity tells a phase from the one before it and the one behind it only,
+  // and when the products lag behind (values on their way) a softmax that waits for the last of them may see two end at once.
+  auto pv_done = [&](int s) { return bars + 8 * (2 * (KK + KV) + 4 + s); };
+  const uint32_t q_ready = bars + 8 * (2 * (KK + KV) + 6), rows_bar = q_ready + 8, end_bar = q_ready + 16;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   clear_dead_rows<bf16>(a, D);
@@ -167,8 +170,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
   if (tid == 0) {
     for (int s = 0; s < KK; ++s) { tc::mbar_init(k_full(s), 1); tc::mbar_init(k_empty(s), 1); }
     for (int s = 0; s < KV; ++s) { tc::mbar_init(v_full(s), 1); tc::mbar_init(v_empty(s), 1); }
-    for (int s = 0; s < 2; ++s) { tc::mbar_init(s_full(s), 1); tc::mbar_init(p_ready(s), 4); }
-    tc::mbar_init(pv_done, 1);
+    for (int s = 0; s < 2; ++s) { tc::mbar_init(s_full(s), 1); tc::mbar_init(p_ready(s), 4); tc::mbar_init(pv_done(s), 1); }
     tc::mbar_init(q_ready, 4);
     tc::mbar_init(rows_bar, 4);
     tc::mbar_init(end_bar, 1);
@@ -233,11 +235,11 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
     if (lane == 0) {
       const uint32_t id_s = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kChunk >> 3) << 17) | ((uint32_t)(kTcRows >> 4) << 24);
       const uint32_t id_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTcRows >> 4) << 24);
-      auto scores = [&](int n, bool first) {
+      auto scores = [&](int n) {
         if (!wait_bar(k_full(n), (n / KK) & 1, dead)) return false;
         // The scores take the place of the weights of two chunks before, whose product must have read them: products are in
-        // order only where they add to the same sums.  (A tile's first chunk comes when all products before it are done.)
-        if (!first && n >= 2 && !wait_bar(pv_done, (n - 2) & 1, dead)) return false;
+        // order only where they add to the same sums.
+        if (n >= 2 && !wait_bar(pv_done(n & 1), ((n - 2) >> 1) & 1, dead)) return false;
         tc::tc_fence_after();
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
@@ -253,10 +255,10 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
         ok = wait_bar(q_ready, tile & 1, dead);
         tc::tc_fence_after();
         const int count = w.c_end - w.c_begin;
-        if (ok) ok = scores(n, true);
+        if (ok) ok = scores(n);
         for (int i = 0; i < count && ok; ++i, ++n) {
           // (the next chunk's scores run ahead, under this one's softmax)
-          if (i + 1 < count && !(ok = scores(n + 1, false))) break;
+          if (i + 1 < count && !(ok = scores(n + 1))) break;
           if (!(ok = wait_bar(p_ready(n & 1), (n >> 1) & 1, dead)) || !(ok = wait_bar(v_full(n), (n / KV) & 1, dead))) break;
           tc::tc_fence_after();
 #pragma unroll
@@ -266,7 +268,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
               umma_f16_ts(o_tmem, tmem + (n & 1) * 64 + plane * 32 + k * 8, value_desc(v_s + n % KV * S::KV_BYTES + k * 2048, S::PANEL), id_o,
                           i > 0 || plane > 0 || k > 0);
           tc::umma_commit(v_empty(n));
-          tc::umma_commit(pv_done);
+          tc::umma_commit(pv_done(n & 1));
         }
         ++tile;
       } while (ok && w.next());
@@ -375,7 +377,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
             m = higher;
             l *= f;
             if (i > 0) {
-              if (!(ok = wait_bar_warp(pv_done, (n - 1) & 1, dead))) break;
+              if (!(ok = wait_bar_warp(pv_done((n - 1) & 1), ((n - 1) >> 1) & 1, dead))) break;
               tc::tc_fence_after();
 #pragma unroll
               for (int d = 0; d < D; d += 32) {
@@ -417,9 +419,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) tree_attention_tc_kernel(const 
       }
       if (!ok) break;
       // ---- the tile's result
-      // (a wait by parity tells a phase from the one before it, not from the one two before: a softmax may be two products ahead)
-      if (count > 1 && !(ok = wait_bar_warp(pv_done, (n - 2) & 1, dead))) break;
-      if (!(ok = wait_bar_warp(pv_done, (n - 1) & 1, dead))) break;
+      if (!(ok = wait_bar_warp(pv_done((n - 1) & 1), ((n - 1) >> 1) & 1, dead))) break;
       tc::tc_fence_after();
       if (tree && !(ok = meet())) break;
       const bool whole = w.whole(), odd = tree && s_odd == tile;
