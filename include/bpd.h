@@ -325,7 +325,15 @@ int bpd_op_linear(const void* x, const void* w, const void* bias, int rows, int 
  * writes a position of it.  capacity = pages_per_row * 64.  Limits (BPD_E_SHAPE
  * beyond them): kv_heads <= 1024, heads <= 4096, batch and layers <= 65535,
  * n_pages <= 2^24, pages_per_row <= 2^20; other head widths are
- * BPD_E_UNSUPPORTED.  A refused call leaves everything as it was. */
+ * BPD_E_UNSUPPORTED.  A refused call leaves everything as it was.
+ *
+ * Outputs overlap no input.  What a row does not see -- positions behind a
+ * length, other nodes -- may hold anything; what it sees counts as it is.  A key
+ * with infinite elements whose score is -inf weighs 0; an infinite or NaN value
+ * leaves no finite output in its column.  Scores, softmax sums and outputs before
+ * their division are held in 32 bits: values above 2^100 may leave that range.
+ * Launches are planned by pages_per_row, not by the lengths on the device: a
+ * table much wider than its rows are long costs short calls 2 to 6 us. */
 typedef struct {
   void* k_pool;               /* device [layers][n_pages][64][kv_heads][head_dim] of dtype, 16-byte aligned */
   void* v_pool;               /* the same for the values; may be NULL where a call only reads keys      */
@@ -397,8 +405,8 @@ int bpd_op_cache_weights(const bpd_cache* cache, const void* q, int nodes, int h
  * tokens), then the largest weights (equal ones: the lower slot; NaN counts as
  * the smallest).  Survivors keep their slots below budget; the holes there, in
  * ascending order, take the survivors above, in ascending order: keys, values,
- * weights and positions move together, what lies at slots >= budget is left as
- * it was.  Slots are then in no order, which attention does not mind and
+ * weights and positions move together (an entry without a page: its weight and
+ * position alone), what lies at slots >= budget is left as it was.  Slots are then in no order, which attention does not mind and
  * `positions` records.  1 <= budget, 0 <= recent <= budget.
  * weights, positions: device [layers][batch][kv_heads][capacity].  out_lens:
  * device [batch]: min(lens, budget); may not overlap lens, seen or the page

@@ -302,8 +302,9 @@ int bpd_op_cache_evict(const bpd_cache* cache, const int32_t* lens, const int32_
   const int lists = a.layers * a.B * a.Hkv;
   a.moves = static_cast<int2*>(scratch); a.moves_cap = moves_cap(cache, budget);
   a.counts = reinterpret_cast<int*>(static_cast<char*>(scratch) + round256((size_t)lists * a.moves_cap * 8));
-  // Up to 128 entries a list move within the launch that selects them (a block over the budget: 522 entries of 48 lists);
-  // more are shared by all SMs in a launch of their own (256 lists of up to 8000: 38 us).
+  // Where a list has room for at most 128 moves they are made by the launch that selects them, else all SMs share them in a launch
+  // of their own.  us with the moves here / shared, entries in L2: 48 lists, 1152 slots to 1024 12.4 / 14.8, 4096 to 256 13.0 / 14.6,
+  // 8000 to 1024 16.7 / 17.6, 8000 to 4000 43 / 31; 256 lists (heads of 128) 17.3 / 18.7, 19.2 / 21.9, 24.0 / 24.2, 89 / 94.
   a.move_here = a.moves_cap <= 128 ? 1 : 0;
   if (a.ppr * kPagePos <= 16 * kEvictThreads) BPD_CUDA(launch_k(cache_evict_kernel<16>, dim3(lists), dim3(kEvictThreads), 0, (cudaStream_t)cuda_stream, false, a));
   else BPD_CUDA(launch_k(cache_evict_kernel<32>, dim3(lists), dim3(kEvictThreads), 0, (cudaStream_t)cuda_stream, false, a));

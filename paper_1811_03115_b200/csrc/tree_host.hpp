@@ -13,11 +13,19 @@ struct AttnPlan {
   int ctas, tile_rows, tiles, combine_rows, split, tc, end_units;   // tiles: that could be
   size_t part_bytes, info_bytes;
 };
-// Tiles of at most so many chunks get a CTA each and need no join: a second launch and its trips to memory cost as much as
-// five chunks (one token over 57 positions 9.0 us with runs, 6.2 with whole tiles; 512 tiles of up to three chunks 19.9 / 14.4;
-// 16 tiles of up to 135 chunks 19 / 98).
+// Tiles of at most so many chunks -- by the table's width, which is all the host knows -- get a CTA each and need no join: a
+// second launch and its trips to memory cost as much as five chunks.  us with runs / with whole tiles, by chunks of a tile:
+//   chunks                              2            3            5            6            7            8            12
+//   bf16, heads of 64, 8 tiles      6.9 / 4.9    7.3 / 5.4    7.5 / 6.7    7.5 / 7.4    7.7 / 8.0    7.7 / 8.6    7.7 / 11.0
+//   bf16, heads of 64, 512 tiles   15.7 / 11.7  16.9 / 13.7  19.6 / 16.9  20.7 / 18.5  22.1 / 19.8  23.2 / 21.5  28.7 / 29.1
+//   bf16, heads of 128, 8 tiles     8.1 / 5.6    8.2 / 6.5    8.7 / 8.2    8.5 / 9.1    8.6 / 10.0   8.6 / 10.8   8.8 / 14.3
+//   fp32, heads of 64, 8 tiles      8.4 / 7.2    8.6 / 8.8    8.7 / 11.9   8.7 / 13.5   8.9 / 14.9   8.9 / 16.5   8.8 / 22.8
+//   fp32, heads of 64, 512 tiles   22.8 / 18.8  26.8 / 23.3  35.9 / 32.5  42.4 / 37.5  46.7 / 43.2  50.7 / 48.5  66.0 / 66.8
 constexpr int kWholeTileChunks = 6;
-// Rows of a tile: as few as hold all rows of a key head, 64 at most.
+// Rows of a tile: as few as hold all rows of a key head, 64 at most.  Over selected pages always 16, a node's heads of one key
+// head at a time: more heads read their pages again, mostly out of L2.  us with tiles of 16 / 32 / 64 rows, 64 nodes and key
+// heads, 32 pages each, bf16 heads of 128: 8 heads to a key head 28 / 32 / 39, 16 31 / 35 / 42, 24 41 / 36 / 44, 32 43 / 38 / 46, 64
+// 60 / 49 / 46 (and from 65 the 128-row kernel); fp32: 8 67 / 105 / 175, 24 116 / 112 / 185.
 inline int tile_rows_of(bool paged, int rows) { return paged || rows <= 16 ? 16 : (rows <= 32 ? 32 : 64); }
 
 template <typename CT> int plan_attention(const AttnArgs& a, bool paged, int D, AttnPlan* plan);
@@ -28,10 +36,11 @@ template <bool PAGED>
 long long max_chunks(const AttnArgs& a) { return (PAGED ? std::min(a.select, a.ppr) + 1 : a.ppr) + ceil_div(a.T, kChunk); }
 
 // A tile's end (its result, the next one's queries, the pipeline's new start) takes as long as some chunks, `cost` of them, and
-// counts as so many where runs are divided: without it, the CTAs that had a tile's end finished last.  Over 8 sequences of 8000,
-// heads of 128, with 0 / 2 / 4 / 8 / 12 chunks: 57.7 / 56.2 / 54.9 / 54.6 / 54.8 us (16 rows), 87.4 / 85.4 / 83.3 / 79.7 / 81.0
-// (128 rows); fp32, 4000 positions, 64 rows: 292 / 286 / 296 / 314 / 326.  Where CTAs have hardly a chunk each it is left out
-// (fp32, 8 heads over 2000 positions: 10.3 us, with it 11.7).
+// counts as so many where runs are divided: without it, the CTAs that had a tile's end finished last.  us with 0 / 2 / 4 / 8 / 12
+// chunks: over 8 sequences of 8000, heads of 128, bf16, 1 row 50.3 / 49.7 / 48.5 / 48.7 / 49.6, 128 rows 89 / 88 / 86 / 82 / 78, heads
+// of 64 128 rows 66 / 64 / 62 / 59 / 60; fp32, 4000 positions, heads of 128, 64 rows 300 / 294 / 299 / 313 / 332, heads of 64 16 rows
+// 45.7 / 43.5 / 44.0 / 46.8 / 48.4.  Where CTAs have hardly a chunk each it is left out (fp32, 8 heads over 2000 positions: 10.5 us,
+// with it 11.4).
 inline int end_units_of(long long units, long long slots, int cost) { return units >= 2 * slots ? cost : 0; }
 
 inline void scratch_of(int D, AttnPlan* p) {
