@@ -212,6 +212,22 @@ def test_tree_attention_of_the_largest_numbers(bpd, lens, nodes, heads, kv_heads
     c.check(out[..., torch.from_numpy(~odd).cuda()], want[..., ~odd], want_lse, lse)
 
 
+# queries that are no numbers, as rows of padding may hold: theirs are the only outputs that show it
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens,nodes,heads,kv_heads,dim", [([70, 5], 3, 2, 2, 64), ([900, 1300], 9, 4, 2, 64), ([900, 0], 40, 2, 1, 128), ([700, 900], 70, 2, 1, 64), ([500], 5, 2, 1, 16)])
+def test_queries_that_are_no_numbers(bpd, lens, nodes, heads, kv_heads, dim, dtype):
+    c = Case(19, lens, nodes, heads, kv_heads, dim, dtype)
+    want, want_lse = plain.attention(c.q, c.k_new[0], c.v_new[0], c.k[0], c.v[0], c.table, c.lens, c.parents, c.nodes, c.scale)
+    _, k_new, v_new = c.drafted()
+    q = c.q.copy()
+    q[:, nodes // 2], q[:, nodes - 1, :, 1] = np.nan, np.nan
+    out, lse = bpd.bpd_op_tree_attention(_dev(q, dtype), k_new, v_new, *c.pools(0), _dev(c.lens), _dev(c.parents), want_lse=True)
+    bad = sorted({nodes // 2, nodes - 1})
+    fine = [t for t in range(nodes) if t not in bad]
+    c.check(out[:, fine], want[:, fine], want_lse[:, fine], lse[:, fine])
+    assert bool(out[:, bad].isnan().all()) and bool(lse[:, bad].isnan().all())
+
+
 # pages outside the pool, parents that do not lie before their node, lengths and node counts outside their ranges
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_values_of_device_arrays_are_not_trusted(bpd, dtype):
