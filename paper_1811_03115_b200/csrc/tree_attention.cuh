@@ -136,7 +136,7 @@ __device__ __forceinline__ void lines_by_warp(Lines& x, const int* parents, int 
       for (int k = 0; k < PER; ++k) d = d && up[k] < 0;
       return d; }());
     if (done) break;
-    __syncwarp();                                           // (a vote orders no memory: this round's reads before the next one's stores)
+    __syncwarp();                                           // (a vote orders no memory: these reads come before the next stores)
   }
   __syncwarp();
 #pragma unroll
